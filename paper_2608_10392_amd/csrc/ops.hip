@@ -1,0 +1,448 @@
+// Host side of the operators around the layer (include/unif_moe_ops.h):
+// argument validation, workspace planning and launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+
+#include "../../include/unif_moe_ops.h"
+#include "balance.hpp"
+#include "common.hpp"
+#include "host.hpp"
+#include "residual.hpp"
+
+using namespace unifmoe;
+
+namespace {
+
+size_t elem_size(int32_t dtype) { return dtype == UNIF_BF16 ? 2 : 4; }
+
+bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+// A tensor as a range of addresses (empty where it is absent).
+struct Span {
+    uintptr_t b, e;
+    Span(const void* p, size_t bytes) : b(reinterpret_cast<uintptr_t>(p)), e(p != nullptr ? b + bytes : b) {}
+    bool meets(const Span& o) const { return b < e && o.b < o.e && b < o.e && o.b < e; }
+    bool same(const Span& o) const { return b == o.b && e == o.e; }
+};
+
+// Whether every output is apart from every input and from the other outputs,
+// but for output i being exactly its partner (an input updated in place).
+template <int NO, int NI>
+bool apart(const Span (&out)[NO], const Span (&partner)[NO], const Span (&in)[NI]) {
+    for (int i = 0; i < NO; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (out[i].meets(out[j])) return false;
+        for (int j = 0; j < NO; ++j)
+            if (out[i].meets(partner[j]) && !(i == j && out[i].same(partner[j]))) return false;
+        for (int j = 0; j < NI; ++j)
+            if (out[i].meets(in[j])) return false;
+    }
+    return true;
+}
+
+bool norm_ok(int32_t norm, float eps, const float* gamma, const float* beta) {
+    if (norm == UNIF_ROWNORM_NONE) return gamma == nullptr && beta == nullptr;
+    if (norm != UNIF_ROWNORM_LAYER && norm != UNIF_ROWNORM_RMS) return false;
+    return eps > 0.0f && std::isfinite(eps) && gamma != nullptr;
+}
+
+int32_t check_residual(const unif_moe_residual* r) {
+    if (r == nullptr) return UNIF_EINVAL;
+    if (r->n_tokens < 0 || r->d_model < 1 || r->tokens_per_gate < 0 || !std::isfinite(r->residual_scale))
+        return UNIF_EINVAL;
+    if (r->dtype != UNIF_F32 && r->dtype != UNIF_BF16) return UNIF_EINVAL;
+    if (r->stream_dtype != UNIF_F32 && (r->stream_dtype != UNIF_BF16 || r->dtype != UNIF_BF16)) return UNIF_EINVAL;
+    if (!norm_ok(r->out_norm, r->out_eps, r->out_gamma, r->out_beta)) return UNIF_EINVAL;
+    if (!norm_ok(r->in_norm, r->in_eps, r->in_gamma, r->in_beta)) return UNIF_EINVAL;
+    for (const float* p : {r->out_gamma, r->out_beta, r->in_gamma, r->in_beta, r->gate})
+        if (!aligned_to(p, 4)) return UNIF_EINVAL;
+    if (r->d_model > UNIF_RESIDUAL_MAX_D) return UNIF_EUNSUPPORTED;
+    return UNIF_OK;
+}
+
+int64_t gate_rows(const unif_moe_residual* r) {
+    if (r->tokens_per_gate == 0) return 1;
+    return ((int64_t)r->n_tokens + r->tokens_per_gate - 1) / r->tokens_per_gate;
+}
+size_t gate_bytes(const unif_moe_residual* r) { return (size_t)gate_rows(r) * r->d_model * sizeof(float); }
+// Several gate rows: their gradients are sums over parts of the tokens.
+bool gate_grouped(const unif_moe_residual* r) { return r->gate != nullptr && gate_rows(r) > 1; }
+
+// Lanes per row (0: the workgroup) and the launch that covers the tokens.
+struct RowShape {
+    int lpr, chunks, threads, rows, blocks;
+    int teams() const { return lpr == 0 ? blocks : blocks * (threads / lpr); }
+};
+RowShape row_shape(int N, int d, int cus) {
+    RowShape s;
+    s.chunks = d > 512 ? 2 : 1;
+    s.lpr = d <= 64 ? 8 : d <= 128 ? 16 : d <= 256 ? 32 : d <= 1024 ? 64 : 0;
+    s.threads = s.lpr == 0 ? ceil_div(d, 1024) * kWave : 256;
+    const int per_block = s.lpr == 0 ? 1 : s.threads / s.lpr;
+    const int most = std::max(1, cus * 8 / (s.threads / kWave)) * per_block;   // teams that run at once
+    s.rows = std::max(1, ceil_div(N, most));
+    s.blocks = ceil_div(ceil_div(N, s.rows), per_block);
+    return s;
+}
+
+// Calls f(shape constants) for the launch's lanes per row.
+template <class F>
+void with_shape(const RowShape& s, F f) {
+    if (s.lpr == 8) f(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
+    else if (s.lpr == 16) f(std::integral_constant<int, 1>(), std::integral_constant<int, 16>());
+    else if (s.lpr == 32) f(std::integral_constant<int, 1>(), std::integral_constant<int, 32>());
+    else if (s.lpr == 64 && s.chunks == 1) f(std::integral_constant<int, 1>(), std::integral_constant<int, 64>());
+    else if (s.lpr == 64) f(std::integral_constant<int, 2>(), std::integral_constant<int, 64>());
+    else f(std::integral_constant<int, 2>(), std::integral_constant<int, 0>());
+}
+
+template <class S, class L>
+void launch_forward(const RowShape& s, const ResidualParams& p, hipStream_t st) {
+    with_shape(s, [&](auto ch, auto lpr) {
+        residual_forward_kernel<S, L, 8, ch.value, lpr.value><<<(unsigned)s.blocks, (unsigned)s.threads, 0, st>>>(p);
+    });
+}
+template <class S, class L, class H>
+void launch_backward(const RowShape& s, const ResidualParams& p, hipStream_t st) {
+    const size_t lds = s.lpr == 0 ? 0 : (size_t)(s.threads / s.lpr) * p.d * sizeof(float);
+    with_shape(s, [&](auto ch, auto lpr) {
+        residual_backward_kernel<S, L, H, 8, ch.value, lpr.value>
+            <<<(unsigned)s.blocks, (unsigned)s.threads, lds, st>>>(p);
+    });
+}
+
+ResidualParams residual_params(const unif_moe_residual* r, const RowShape& s) {
+    ResidualParams p{};
+    p.N = r->n_tokens;
+    p.d = r->d_model;
+    p.rows = s.rows;
+    p.out_norm = r->out_norm;
+    p.in_norm = r->in_norm;
+    p.group = gate_grouped(r) ? r->tokens_per_gate : r->n_tokens;
+    p.out_eps = r->out_eps;
+    p.in_eps = r->in_eps;
+    p.scale = r->residual_scale;
+    p.inv_d = (float)(1.0 / r->d_model);
+    p.out_gamma = r->out_gamma;
+    p.out_beta = r->out_beta;
+    p.in_gamma = r->in_gamma;
+    p.in_beta = r->in_beta;
+    p.gate = r->gate;
+    return p;
+}
+
+// Workspace of the backward: partial rows of the five parameters per workgroup
+// and a team's two pieces of shared gate groups, for the launch of any number
+// of compute units up to kMaxCus (the size is known without a device).
+constexpr int kMaxCus = 512;
+struct ResidualPlan {
+    size_t part, gate_part, total;
+};
+ResidualPlan plan_residual(const unif_moe_residual* r) {
+    const RowShape s = row_shape(r->n_tokens, r->d_model, kMaxCus);
+    const size_t row = (size_t)r->d_model * sizeof(float);
+    Carver cv;
+    ResidualPlan p;
+    p.part = cv.take(5 * row * s.blocks);
+    p.gate_part = cv.take(gate_grouped(r) ? 2 * row * s.teams() : 0);
+    p.total = cv.cur + 256;
+    return p;
+}
+
+__global__ void zero_floats_kernel(float* p, size_t n) {
+    for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (size_t)gridDim.x * blockDim.x) p[i] = 0.f;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t unif_moe_residual_forward(const unif_moe_residual* res, const void* x, const void* f, const uint8_t* valid,
+                                  void* y, void* h, void* stream) {
+    const int32_t s = check_residual(res);
+    if (s != UNIF_OK) return s;
+    const size_t n = (size_t)res->n_tokens * res->d_model;
+    const size_t se = elem_size(res->stream_dtype), le = elem_size(res->dtype);
+    if (n > 0) {
+        if ((x == nullptr && f == nullptr) || (y == nullptr && h == nullptr)) return UNIF_EINVAL;
+        if (f == nullptr && (res->out_norm != UNIF_ROWNORM_NONE || res->gate != nullptr)) return UNIF_EINVAL;
+    }
+    if (h != nullptr && res->in_norm == UNIF_ROWNORM_NONE) return UNIF_EINVAL;
+    if (!aligned_to(x, se) || !aligned_to(y, se) || !aligned_to(f, le) || !aligned_to(h, le)) return UNIF_EINVAL;
+    const size_t row = (size_t)res->d_model * 4;
+    const Span out[] = {Span(y, n * se), Span(h, n * le)}, partner[] = {Span(x, n * se), Span(nullptr, 0)};
+    const Span in[] = {Span(f, n * le), Span(valid, res->n_tokens), Span(res->out_gamma, row),
+                       Span(res->out_beta, row), Span(res->in_gamma, row), Span(res->in_beta, row),
+                       Span(res->gate, gate_bytes(res))};
+    if (!apart(out, partner, in)) return UNIF_EINVAL;
+    if (n == 0) return UNIF_OK;
+    const RowShape sh = row_shape(res->n_tokens, res->d_model, std::min(cu_count(), kMaxCus));
+    ResidualParams p = residual_params(res, sh);
+    p.x = x;
+    p.f = f;
+    p.valid = valid;
+    p.y = y;
+    p.h = h;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (res->dtype == UNIF_F32) launch_forward<float, float>(sh, p, st);
+    else if (res->stream_dtype == UNIF_F32) launch_forward<float, u16>(sh, p, st);
+    else launch_forward<u16, u16>(sh, p, st);
+    UNIF_LAUNCH_CHECK();
+    return UNIF_OK;
+}
+
+int32_t unif_moe_residual_backward_workspace_size(const unif_moe_residual* res, size_t* bytes) {
+    if (bytes == nullptr) return UNIF_EINVAL;
+    const int32_t s = check_residual(res);
+    if (s != UNIF_OK) return s;
+    *bytes = plan_residual(res).total;
+    return UNIF_OK;
+}
+
+int32_t unif_moe_residual_backward(const unif_moe_residual* res, const void* y, const void* f, const uint8_t* valid,
+                                   const void* dy, const void* dh, int32_t dh_dtype, void* dx, void* df,
+                                   const unif_moe_residual_grads* grads, void* workspace, size_t workspace_bytes,
+                                   void* stream) {
+    const int32_t s = check_residual(res);
+    if (s != UNIF_OK) return s;
+    if (dh_dtype != UNIF_F32 && dh_dtype != res->dtype) return UNIF_EINVAL;
+    static const unif_moe_residual_grads none{};
+    const unif_moe_residual_grads& gr = grads != nullptr ? *grads : none;
+    float* const want[5] = {gr.out_gamma, gr.out_beta, gr.in_gamma, gr.in_beta, gr.gate};
+    const float* const have[5] = {res->out_gamma, res->out_beta, res->in_gamma, res->in_beta, res->gate};
+    for (int i = 0; i < 5; ++i)
+        if (want[i] != nullptr && (have[i] == nullptr || !aligned_to(want[i], 4))) return UNIF_EINVAL;
+    const size_t n = (size_t)res->n_tokens * res->d_model;
+    const size_t se = elem_size(res->stream_dtype), le = elem_size(res->dtype), he = elem_size(dh_dtype);
+    if (n > 0) {
+        if (dy == nullptr && dh == nullptr) return UNIF_EINVAL;
+        if ((dh == nullptr) != (y == nullptr)) return UNIF_EINVAL;
+        if (dh == nullptr && (gr.in_gamma != nullptr || gr.in_beta != nullptr)) return UNIF_EINVAL;
+        const bool branch = gr.out_gamma != nullptr || gr.out_beta != nullptr || gr.gate != nullptr ||
+                            (df != nullptr && res->out_norm != UNIF_ROWNORM_NONE);
+        if (branch && f == nullptr) return UNIF_EINVAL;
+    }
+    if (dh != nullptr && res->in_norm == UNIF_ROWNORM_NONE) return UNIF_EINVAL;
+    if (!aligned_to(y, se) || !aligned_to(dy, se) || !aligned_to(dx, se) || !aligned_to(f, le) ||
+        !aligned_to(df, le) || !aligned_to(dh, he))
+        return UNIF_EINVAL;
+    const ResidualPlan plan = plan_residual(res);
+    if (workspace == nullptr || workspace_bytes < plan.total) return UNIF_EWORKSPACE;
+    const size_t row = (size_t)res->d_model * 4, gb = gate_bytes(res);
+    const Span out[] = {Span(dx, n * se), Span(df, n * le), Span(gr.out_gamma, row), Span(gr.out_beta, row),
+                        Span(gr.in_gamma, row), Span(gr.in_beta, row), Span(gr.gate, gb),
+                        Span(workspace, plan.total)};
+    const Span no(nullptr, 0);
+    const Span partner[] = {Span(dy, n * se), no, no, no, no, no, no, no};
+    const Span in[] = {Span(y, n * se), Span(f, n * le), Span(valid, res->n_tokens), Span(dh, n * he),
+                       Span(res->out_gamma, row), Span(res->out_beta, row), Span(res->in_gamma, row),
+                       Span(res->in_beta, row), Span(res->gate, gb)};
+    if (!apart(out, partner, in)) return UNIF_EINVAL;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (n == 0) {   // sums over no tokens
+        for (int i = 0; i < 5; ++i) {
+            const size_t m = i == 4 ? gb / 4 : (size_t)res->d_model;
+            if (want[i] == nullptr || m == 0) continue;
+            zero_floats_kernel<<<(unsigned)std::min<size_t>(ceil_div_sz(m, 256), 1024), 256, 0, st>>>(want[i], m);
+            UNIF_LAUNCH_CHECK();
+        }
+        return UNIF_OK;
+    }
+    const RowShape sh = row_shape(res->n_tokens, res->d_model, std::min(cu_count(), kMaxCus));
+    ResidualParams p = residual_params(res, sh);
+    char* ws = align_base(workspace);
+    const bool grouped = gr.gate != nullptr && gate_grouped(res);
+    p.x = y;
+    p.f = f;
+    p.valid = valid;
+    p.dy = dy;
+    p.dh = dh;
+    p.dx = dx;
+    p.df = df;
+    p.part = reinterpret_cast<float*>(ws + plan.part);
+    p.gate_part = reinterpret_cast<float*>(ws + plan.gate_part);
+    p.dgate = grouped ? gr.gate : nullptr;
+    ResidualSums sums{};
+    sums.d = p.d;
+    sums.parts = sh.blocks;
+    sums.part = p.part;
+    for (int i = 0; i < 5; ++i)
+        if (want[i] != nullptr && !(i == 4 && grouped)) {
+            p.want |= 1 << i;
+            sums.out[i] = want[i];
+        }
+    if (res->dtype == UNIF_F32) launch_backward<float, float, float>(sh, p, st);
+    else if (res->stream_dtype == UNIF_F32 && dh_dtype == UNIF_F32) launch_backward<float, u16, float>(sh, p, st);
+    else if (res->stream_dtype == UNIF_F32) launch_backward<float, u16, u16>(sh, p, st);
+    else if (dh_dtype == UNIF_F32) launch_backward<u16, u16, float>(sh, p, st);
+    else launch_backward<u16, u16, u16>(sh, p, st);
+    UNIF_LAUNCH_CHECK();
+    if (p.want != 0) {
+        residual_param_sum_kernel<<<dim3((unsigned)ceil_div(p.d, 64), 5), 256, 0, st>>>(sums);
+        UNIF_LAUNCH_CHECK();
+    }
+    if (grouped && sh.teams() > 1) {
+        ResidualGates g{p.N, p.d, p.group, p.rows, p.gate_part, p.dgate};
+        residual_gate_join_kernel<<<dim3((unsigned)ceil_div(p.d, 256), (unsigned)(sh.teams() - 1)), 256, 0, st>>>(g);
+        UNIF_LAUNCH_CHECK();
+    }
+    return UNIF_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+int32_t check_balance(const unif_moe_config* c, const unif_moe_balance* b) {
+    const int32_t s = check_config(c);
+    if (s != UNIF_OK) return s;
+    if (b == nullptr || b->tokens_per_group < 0 || !std::isfinite(b->weight)) return UNIF_EINVAL;
+    if (b->unit != UNIF_BALANCE_TOKENS && b->unit != UNIF_BALANCE_BLOCKS) return UNIF_EINVAL;
+    return UNIF_OK;
+}
+
+constexpr int kBalPiece = 256;    // tokens per piece of a group
+constexpr int kBalSlices = 64;
+
+struct BalanceShape {
+    int group, groups, pieces;
+};
+BalanceShape balance_shape(const unif_moe_config* c, const unif_moe_balance* b) {
+    BalanceShape s;
+    s.group = b->tokens_per_group > 0 ? b->tokens_per_group : std::max(c->n_tokens, 1);
+    s.groups = b->tokens_per_group > 0 ? ceil_div(c->n_tokens, s.group) : 1;
+    s.pieces = ceil_div(std::min(s.group, std::max(c->n_tokens, 1)), kBalPiece);
+    return s;
+}
+
+struct BalancePlan {
+    size_t mass, load, slope, gloss, dl, part, total;
+};
+BalancePlan plan_balance(const unif_moe_config* c, const unif_moe_balance* b) {
+    const BalanceShape s = balance_shape(c, b);
+    const size_t K = c->n_experts, units = (size_t)s.groups * s.pieces;
+    Carver cv;
+    BalancePlan p;
+    p.mass = cv.take(4 * units * K);
+    p.load = cv.take(4 * units * (K + 2));
+    p.slope = cv.take(4 * s.groups * K);
+    p.gloss = cv.take(8 * (size_t)s.groups);
+    p.dl = cv.take(4 * K * c->n_tokens);
+    p.part = cv.take(4 * (size_t)kBalSlices * K * c->d_model);
+    p.total = cv.cur + 256;
+    return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t unif_moe_balance_loss_workspace_size(const unif_moe_config* cfg, const unif_moe_balance* bal, size_t* bytes) {
+    if (bytes == nullptr) return UNIF_EINVAL;
+    const int32_t s = check_balance(cfg, bal);
+    if (s != UNIF_OK) return s;
+    *bytes = plan_balance(cfg, bal).total;
+    return UNIF_OK;
+}
+
+int32_t unif_moe_balance_loss(const unif_moe_config* cfg, const unif_moe_balance* bal, const unif_moe_routing* record,
+                              const uint8_t* valid, const void* X, const float* W_router, float* loss, int64_t* counts,
+                              const float* dX_in, float* dX, const float* dW_router_in, float* dW_router,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+    const int32_t s = check_balance(cfg, bal);
+    if (s != UNIF_OK) return s;
+    const int N = cfg->n_tokens, d = cfg->d_model, K = cfg->n_experts;
+    if (loss == nullptr) return UNIF_EINVAL;
+    if (N > 0 && (!record_complete(record) || (dX != nullptr && W_router == nullptr) ||
+                  (dW_router != nullptr && X == nullptr)))
+        return UNIF_EINVAL;
+    if ((dX == nullptr && dX_in != nullptr) || (dW_router == nullptr && dW_router_in != nullptr)) return UNIF_EINVAL;
+    if (!aligned_to(X, elem_size(cfg->dtype)) || !aligned_to(counts, 8)) return UNIF_EINVAL;
+    for (const void* q : {(const void*)W_router, (const void*)loss, (const void*)dX_in, (const void*)dX,
+                          (const void*)dW_router_in, (const void*)dW_router})
+        if (!aligned_to(q, 4)) return UNIF_EINVAL;
+    const BalancePlan plan = plan_balance(cfg, bal);
+    if (workspace == nullptr || workspace_bytes < plan.total) return UNIF_EWORKSPACE;
+    const BalanceShape sh = balance_shape(cfg, bal);
+    const size_t nd = (size_t)N * d, wb = 4 * (size_t)(K + 1) * d;
+    static const unif_moe_routing no_record{};
+    const unif_moe_routing& rec = N > 0 ? *record : no_record;
+    const Span no(nullptr, 0);
+    const Span out[] = {Span(loss, 4), Span(counts, 8 * (size_t)sh.groups * (K + 1)), Span(dX, 4 * nd),
+                        Span(dW_router, wb), Span(workspace, plan.total)};
+    const Span partner[] = {no, no, Span(dX_in, 4 * nd), Span(dW_router_in, wb), no};
+    const Span in[] = {Span(valid, N), Span(X, nd * elem_size(cfg->dtype)), Span(W_router, wb),
+                       Span(rec.n_shared, 4 * (size_t)N), Span(rec.n_res, 4 * (size_t)N),
+                       Span(rec.expert_ids, 4 * (size_t)N * K), Span(rec.weights, 4 * (size_t)N * K)};
+    if (!apart(out, partner, in)) return UNIF_EINVAL;
+    char* ws = align_base(workspace);
+    BalanceParams p{};
+    p.N = N;
+    p.d = d;
+    p.K = K;
+    p.B = cfg->n_blocks;
+    p.group = sh.group;
+    p.groups = sh.groups;
+    p.pieces = sh.pieces;
+    p.piece = kBalPiece;
+    p.blocks = bal->unit == UNIF_BALANCE_BLOCKS;
+    p.weight = bal->weight;
+    p.valid = valid;
+    p.nsh = rec.n_shared;
+    p.nres = rec.n_res;
+    p.eids = rec.expert_ids;
+    p.wts = rec.weights;
+    p.X = X;
+    p.Wr = W_router;
+    p.dX_in = dX_in;
+    p.dX = dX;
+    p.dW_in = dW_router_in;
+    p.dW = dW_router;
+    p.loss = loss;
+    p.counts = counts;
+    p.mass = reinterpret_cast<float*>(ws + plan.mass);
+    p.load = reinterpret_cast<int*>(ws + plan.load);
+    p.slope = reinterpret_cast<float*>(ws + plan.slope);
+    p.gloss = reinterpret_cast<double*>(ws + plan.gloss);
+    p.dl = reinterpret_cast<float*>(ws + plan.dl);
+    p.part = reinterpret_cast<float*>(ws + plan.part);
+    p.slices = N > 0 ? kBalSlices : 0;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (sh.groups > 0) {
+        const int64_t units = (int64_t)sh.groups * sh.pieces;
+        const size_t lds = sizeof(float) * kBalWaves * (size_t)balance_lds_words(K);
+        if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(balance_count_kernel),
+                                                   hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
+            return UNIF_EDEVICE;
+        balance_count_kernel<<<(unsigned)((units + kBalWaves - 1) / kBalWaves), 64 * kBalWaves, lds, st>>>(p);
+        UNIF_LAUNCH_CHECK();
+        balance_group_kernel<<<(unsigned)sh.groups, 64, 0, st>>>(p);
+        UNIF_LAUNCH_CHECK();
+    }
+    balance_loss_kernel<<<1, 256, 0, st>>>(p);
+    UNIF_LAUNCH_CHECK();
+    if (N > 0 && (dX != nullptr || dW_router != nullptr)) {
+        balance_dl_kernel<<<(unsigned)ceil_div(N, 256), 256, 0, st>>>(p);
+        UNIF_LAUNCH_CHECK();
+    }
+    if (N > 0 && dX != nullptr) {
+        balance_dx_kernel<<<dim3((unsigned)ceil_div(N, 16), (unsigned)ceil_div(d, 256)), 256, 0, st>>>(p);
+        UNIF_LAUNCH_CHECK();
+    }
+    if (dW_router != nullptr) {
+        if (N > 0) {
+            const dim3 grid((unsigned)ceil_div(d, 256), (unsigned)ceil_div(K, 8), kBalSlices);
+            if (cfg->dtype == UNIF_BF16) balance_dw_kernel<u16><<<grid, 256, 0, st>>>(p);
+            else balance_dw_kernel<float><<<grid, 256, 0, st>>>(p);
+            UNIF_LAUNCH_CHECK();
+        }
+        balance_dw_sum_kernel<<<(unsigned)ceil_div_sz((size_t)(K + 1) * d, 256), 256, 0, st>>>(p);
+        UNIF_LAUNCH_CHECK();
+    }
+    return UNIF_OK;
+}
+
+}  // extern "C"

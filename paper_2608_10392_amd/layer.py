@@ -2,14 +2,17 @@
 and calls the HIP library on them (torch supplies memory and streams)."""
 import numpy as np
 
-from . import _lib
+from . import _lib, ops
 
 
 def to_device(a, dtype_name, device):
-    """numpy array -> torch device tensor; bf16 data arrives as uint16 bits."""
+    """numpy array -> torch device tensor; bf16 data arrives as uint16 bits.
+    Tensors are moved as they are."""
     import torch
     if a is None:
         return None
+    if torch.is_tensor(a):
+        return a.to(device)
     if dtype_name == "bf16":
         t = torch.from_numpy(np.ascontiguousarray(a).view(np.int16)).view(torch.bfloat16)
     else:
@@ -86,6 +89,29 @@ class DeviceLayer:
                             stream=stream)
         return g
 
+    def diversity_loss(self, weight, dW_router, stream=None):
+        """L_div of the router as a device scalar; weight times its gradient is
+        added to ``dW_router``."""
+        import torch
+        loss = torch.empty(1, dtype=torch.float32, device=self.device)
+        ws = _lib.alloc_workspace(_lib.diversity_loss_workspace_size(self.cfg), self.device)
+        _lib.diversity_loss(self.cfg, self.W_router, weight, loss, dW_router, ws, stream=stream)
+        return loss
+
+    def balance_loss(self, bal, dX=None, dW_router=None, stream=None):
+        """Balance loss and per-expert loads (device tensors) over the routing
+        record of the last forward or route; weight times the loss's gradient is
+        added to ``dX`` and ``dW_router`` where given."""
+        import torch
+        c = self.cfg
+        rows = ops.gate_rows(c["n_tokens"], bal.get("tokens_per_group", 0))
+        loss = torch.empty(1, dtype=torch.float32, device=self.device)
+        counts = torch.empty((rows, c["n_experts"] + 1), dtype=torch.int64, device=self.device)
+        ws = _lib.alloc_workspace(ops.balance_loss_workspace_size(c, bal), self.device)
+        ops.balance_loss(c, bal, self.routing, self.valid, self.X, self.W_router, loss, counts, dX, dX, dW_router,
+                         dW_router, ws, stream=stream)
+        return loss, counts
+
     def route(self, out=None, stream=None):
         if self.ws_route is None:
             self.ws_route = _lib.alloc_workspace(_lib.route_workspace_size(self.cfg), self.device)
@@ -109,3 +135,56 @@ class DeviceLayer:
         if self.cfg["dtype"] == "bf16":
             return self.Y.view(torch.int16).cpu().numpy().view(np.uint16)
         return self.Y.cpu().numpy()
+
+
+class DeviceBlock:
+    """A block around the layer in training: y = residual_scale x + gate
+    N_out(F(N_in(x))), with F the layer, and the gradients of a loss of y with
+    the balance loss and the diversity loss added.
+
+    ``params`` is the join's description (ops.make_residual) without sizes and
+    types; its in_norm belongs to N_in in front of the layer, the rest to the
+    join behind it. ``stream_dtype`` is the residual stream's type.
+    """
+
+    def __init__(self, layer, params, stream_dtype=None):
+        import torch
+        self.layer, self.params = layer, dict(params)
+        c = layer.cfg
+        size = dict(n_tokens=c["n_tokens"], d_model=c["d_model"], dtype=c["dtype"],
+                    stream_dtype=stream_dtype or c["dtype"])
+        before = {k: v for k, v in params.items() if k in ("in_norm", "in_eps", "in_gamma", "in_beta")}
+        behind = {k: v for k, v in params.items() if k not in before}
+        self.before = ops.make_residual(dict(size, **before))
+        self.behind = ops.make_residual(dict(size, **behind))
+        self.stream = torch.bfloat16 if size["stream_dtype"] == "bf16" else torch.float32
+
+    def forward(self, x, stream=None):
+        import torch
+        L = self.layer
+        L.X = torch.empty((L.cfg["n_tokens"], L.cfg["d_model"]), dtype=L.Y.dtype, device=L.device)
+        ops.residual_forward(self.before, x, None, L.valid, None, L.X, stream=stream)
+        f = L.forward(stream=stream)
+        y = torch.empty_like(x)
+        ops.residual_forward(self.behind, x, f, L.valid, y, None, stream=stream)
+        return y
+
+    def backward(self, x, dy, balance=None, diversity=0.0, stream=None):
+        """Gradients of the last forward: dx, the layer's (dW_up, dW_down,
+        dW_router) and the parameters', and the losses."""
+        import torch
+        L = self.layer
+        like = {k: torch.empty_like(v) for k, v in self.params.items() if k in ops.PARAMS and v is not None}
+        df, dx = torch.empty_like(L.Y), torch.empty_like(dy)
+        ws = [_lib.alloc_workspace(ops.residual_backward_workspace_size(r), L.device)
+              for r in (self.behind, self.before)]
+        ops.residual_backward(self.behind, None, L.Y, L.valid, dy, None, dx, df,
+                              {k: v for k, v in like.items() if not k.startswith("in_")}, ws[0], stream=stream)
+        g = L.backward(df, stream=stream)
+        if balance is not None:
+            g["balance"], g["counts"] = L.balance_loss(balance, g["dX"], g["dW_router"], stream=stream)
+        if diversity:
+            g["diversity"] = L.diversity_loss(diversity, g["dW_router"], stream=stream)
+        ops.residual_backward(self.before, x, None, L.valid, dx, g.pop("dX"), dx, None,
+                              {k: v for k, v in like.items() if k.startswith("in_")}, ws[1], stream=stream)
+        return dict(g, dx=dx, **like)
