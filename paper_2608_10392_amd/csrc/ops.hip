@@ -76,40 +76,59 @@ struct RowShape {
     int lpr, chunks, threads, rows, blocks;
     int teams() const { return lpr == 0 ? blocks : blocks * (threads / lpr); }
 };
-RowShape row_shape(int N, int d, int cus) {
+// 3 or 4 chunks of E columns per lane, the fewer that cover the row; rows of
+// more than one wave's 1,024 columns take a workgroup.
+RowShape row_shape(int N, int d, int cus, int waves_per_cu) {
     RowShape s;
-    s.chunks = d > 512 ? 2 : 1;
-    s.lpr = d <= 64 ? 8 : d <= 128 ? 16 : d <= 256 ? 32 : d <= 1024 ? 64 : 0;
-    s.threads = s.lpr == 0 ? ceil_div(d, 1024) * kWave : 256;
+    s.lpr = 8;
+    while (s.lpr < kWave && s.lpr * 4 * E < d) s.lpr *= 2;
+    s.threads = 256;
+    if (s.lpr * 4 * E >= d) {
+        s.chunks = s.lpr * 3 * E >= d ? 3 : 4;
+    } else {
+        s.lpr = 0;
+        const int w3 = ceil_div(d, kWave * 3 * E), w4 = ceil_div(d, kWave * 4 * E);
+        s.chunks = w3 * 3 < w4 * 4 && w3 <= kWideWaves ? 3 : 4;
+        s.threads = (s.chunks == 3 ? w3 : w4) * kWave;
+    }
     const int per_block = s.lpr == 0 ? 1 : s.threads / s.lpr;
-    const int most = std::max(1, cus * 8 / (s.threads / kWave)) * per_block;   // teams that run at once
+    const int most = std::max(1, cus * waves_per_cu / (s.threads / kWave)) * per_block;   // teams of a full chip
     s.rows = std::max(1, ceil_div(N, most));
     s.blocks = ceil_div(ceil_div(N, s.rows), per_block);
     return s;
 }
 
-// Calls f(shape constants) for the launch's lanes per row.
+// Calls f(chunks, lanes per row) for a launch's shape.
+template <int CH, class F>
+void with_lanes(const RowShape& s, F f) {
+    const std::integral_constant<int, CH> ch;
+    switch (s.lpr) {
+        case 8: return f(ch, std::integral_constant<int, 8>());
+        case 16: return f(ch, std::integral_constant<int, 16>());
+        case 32: return f(ch, std::integral_constant<int, 32>());
+        case 64: return f(ch, std::integral_constant<int, 64>());
+        default: return f(ch, std::integral_constant<int, 0>());
+    }
+}
 template <class F>
 void with_shape(const RowShape& s, F f) {
-    if (s.lpr == 8) f(std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
-    else if (s.lpr == 16) f(std::integral_constant<int, 1>(), std::integral_constant<int, 16>());
-    else if (s.lpr == 32) f(std::integral_constant<int, 1>(), std::integral_constant<int, 32>());
-    else if (s.lpr == 64 && s.chunks == 1) f(std::integral_constant<int, 1>(), std::integral_constant<int, 64>());
-    else if (s.lpr == 64) f(std::integral_constant<int, 2>(), std::integral_constant<int, 64>());
-    else f(std::integral_constant<int, 2>(), std::integral_constant<int, 0>());
+    if (s.chunks == 3) with_lanes<3>(s, f);
+    else with_lanes<4>(s, f);
 }
+
+constexpr int kForwardWaves = 16, kBackwardWaves = 8;   // per compute unit
 
 template <class S, class L>
 void launch_forward(const RowShape& s, const ResidualParams& p, hipStream_t st) {
     with_shape(s, [&](auto ch, auto lpr) {
-        residual_forward_kernel<S, L, 8, ch.value, lpr.value><<<(unsigned)s.blocks, (unsigned)s.threads, 0, st>>>(p);
+        residual_forward_kernel<S, L, ch.value, lpr.value><<<(unsigned)s.blocks, (unsigned)s.threads, 0, st>>>(p);
     });
 }
 template <class S, class L, class H>
 void launch_backward(const RowShape& s, const ResidualParams& p, hipStream_t st) {
-    const size_t lds = s.lpr == 0 ? 0 : (size_t)(s.threads / s.lpr) * p.d * sizeof(float);
+    const size_t lds = (size_t)(s.teams() / s.blocks) * 2 * p.d * sizeof(float);
     with_shape(s, [&](auto ch, auto lpr) {
-        residual_backward_kernel<S, L, H, 8, ch.value, lpr.value>
+        residual_backward_kernel<S, L, H, ch.value, lpr.value>
             <<<(unsigned)s.blocks, (unsigned)s.threads, lds, st>>>(p);
     });
 }
@@ -134,7 +153,7 @@ ResidualParams residual_params(const unif_moe_residual* r, const RowShape& s) {
     return p;
 }
 
-// Workspace of the backward: partial rows of the five parameters per workgroup
+// Workspace of the backward: four partial rows per workgroup
 // and a team's two pieces of shared gate groups, for the launch of any number
 // of compute units up to kMaxCus (the size is known without a device).
 constexpr int kMaxCus = 512;
@@ -142,11 +161,11 @@ struct ResidualPlan {
     size_t part, gate_part, total;
 };
 ResidualPlan plan_residual(const unif_moe_residual* r) {
-    const RowShape s = row_shape(r->n_tokens, r->d_model, kMaxCus);
+    const RowShape s = row_shape(r->n_tokens, r->d_model, kMaxCus, kBackwardWaves);
     const size_t row = (size_t)r->d_model * sizeof(float);
     Carver cv;
     ResidualPlan p;
-    p.part = cv.take(5 * row * s.blocks);
+    p.part = cv.take(4 * row * s.blocks);
     p.gate_part = cv.take(gate_grouped(r) ? 2 * row * s.teams() : 0);
     p.total = cv.cur + 256;
     return p;
@@ -179,7 +198,7 @@ int32_t unif_moe_residual_forward(const unif_moe_residual* res, const void* x, c
                        Span(res->gate, gate_bytes(res))};
     if (!apart(out, partner, in)) return UNIF_EINVAL;
     if (n == 0) return UNIF_OK;
-    const RowShape sh = row_shape(res->n_tokens, res->d_model, std::min(cu_count(), kMaxCus));
+    const RowShape sh = row_shape(res->n_tokens, res->d_model, std::min(cu_count(), kMaxCus), kForwardWaves);
     ResidualParams p = residual_params(res, sh);
     p.x = x;
     p.f = f;
@@ -251,10 +270,10 @@ int32_t unif_moe_residual_backward(const unif_moe_residual* res, const void* y, 
         }
         return UNIF_OK;
     }
-    const RowShape sh = row_shape(res->n_tokens, res->d_model, std::min(cu_count(), kMaxCus));
+    const RowShape sh = row_shape(res->n_tokens, res->d_model, std::min(cu_count(), kMaxCus), kBackwardWaves);
     ResidualParams p = residual_params(res, sh);
     char* ws = align_base(workspace);
-    const bool grouped = gr.gate != nullptr && gate_grouped(res);
+    p.grouped = gate_grouped(res);
     p.x = y;
     p.f = f;
     p.valid = valid;
@@ -264,29 +283,24 @@ int32_t unif_moe_residual_backward(const unif_moe_residual* res, const void* y, 
     p.df = df;
     p.part = reinterpret_cast<float*>(ws + plan.part);
     p.gate_part = reinterpret_cast<float*>(ws + plan.gate_part);
-    p.dgate = grouped ? gr.gate : nullptr;
-    ResidualSums sums{};
-    sums.d = p.d;
-    sums.parts = sh.blocks;
-    sums.part = p.part;
-    for (int i = 0; i < 5; ++i)
-        if (want[i] != nullptr && !(i == 4 && grouped)) {
-            p.want |= 1 << i;
-            sums.out[i] = want[i];
-        }
+    p.dgate = p.grouped ? gr.gate : nullptr;
+    const bool one_gate = !p.grouped && gr.gate != nullptr;   // from the sums of out_gamma and out_beta
+    p.want = (gr.out_gamma != nullptr || one_gate ? 1 << kSumOutGamma : 0) |
+             (gr.out_beta != nullptr || one_gate ? 1 << kSumOutBeta : 0) |
+             (gr.in_gamma != nullptr ? 1 << kSumInGamma : 0) | (gr.in_beta != nullptr ? 1 << kSumInBeta : 0);
     if (res->dtype == UNIF_F32) launch_backward<float, float, float>(sh, p, st);
     else if (res->stream_dtype == UNIF_F32 && dh_dtype == UNIF_F32) launch_backward<float, u16, float>(sh, p, st);
     else if (res->stream_dtype == UNIF_F32) launch_backward<float, u16, u16>(sh, p, st);
     else if (dh_dtype == UNIF_F32) launch_backward<u16, u16, float>(sh, p, st);
     else launch_backward<u16, u16, u16>(sh, p, st);
     UNIF_LAUNCH_CHECK();
-    if (p.want != 0) {
-        residual_param_sum_kernel<<<dim3((unsigned)ceil_div(p.d, 64), 5), 256, 0, st>>>(sums);
-        UNIF_LAUNCH_CHECK();
-    }
-    if (grouped && sh.teams() > 1) {
-        ResidualGates g{p.N, p.d, p.group, p.rows, p.gate_part, p.dgate};
-        residual_gate_join_kernel<<<dim3((unsigned)ceil_div(p.d, 256), (unsigned)(sh.teams() - 1)), 256, 0, st>>>(g);
+    if (p.want != 0 || p.dgate != nullptr) {
+        const ResidualFinish fin{p.N, p.d, sh.blocks, sh.teams(), p.group, p.rows, gate_rows(res), p.grouped, p.part,
+                                 p.gate_part, res->out_gamma, res->out_beta, res->gate, gr.out_gamma, gr.out_beta,
+                                 gr.in_gamma, gr.in_beta, gr.gate};
+        const int64_t shared = p.dgate != nullptr ? std::min<int64_t>(sh.teams() - 1, gate_rows(res)) : 0;
+        residual_finish_kernel<<<dim3((unsigned)ceil_div(p.d, kWave), (unsigned)(2 + shared)), kFinishWaves * kWave, 0,
+                                 st>>>(fin);
         UNIF_LAUNCH_CHECK();
     }
     return UNIF_OK;
