@@ -36,7 +36,8 @@ extern "C" {
 #define UNIF_ROWNORM_LAYER 1
 #define UNIF_ROWNORM_RMS   2
 
-/* Widest rows of the residual operators. */
+/* Narrowest and widest rows of the residual operators. */
+#define UNIF_RESIDUAL_MIN_D 4
 #define UNIF_RESIDUAL_MAX_D 8192
 
 /* The join of a block's branch f with the residual stream x, and the norm in
@@ -44,7 +45,7 @@ extern "C" {
  *   v = residual_scale * x + gate * N_out(f),   y = v,   h = N_in(v). */
 typedef struct unif_moe_residual {
     int32_t n_tokens;        /* N >= 0 rows                                          */
-    int32_t d_model;         /* d in [1, UNIF_RESIDUAL_MAX_D]                        */
+    int32_t d_model;         /* d in [UNIF_RESIDUAL_MIN_D, UNIF_RESIDUAL_MAX_D]      */
     int32_t dtype;           /* UNIF_F32 or UNIF_BF16: f, h and df (what the layer
                                 takes and returns)                                   */
     int32_t stream_dtype;    /* x, y, dy and dx: UNIF_F32, or UNIF_BF16 where dtype
@@ -77,7 +78,7 @@ typedef struct unif_moe_residual {
  * Precision: sums, statistics and the row itself in fp32; y and h are each
  * rounded once (h is formed from the unrounded v). Values beyond about 1e18
  * in magnitude overflow the statistics.
- * Errors: UNIF_EINVAL, UNIF_EUNSUPPORTED (d > UNIF_RESIDUAL_MAX_D) before any
+ * Errors: UNIF_EINVAL, UNIF_EUNSUPPORTED (d out of range) before any
  * launch; UNIF_EDEVICE if a launch fails. */
 int32_t unif_moe_residual_forward(const unif_moe_residual* res, const void* x, const void* f,
                                   const uint8_t* valid, void* y, void* h, void* stream);

@@ -59,7 +59,7 @@ int32_t check_residual(const unif_moe_residual* r) {
     if (!norm_ok(r->in_norm, r->in_eps, r->in_gamma, r->in_beta)) return UNIF_EINVAL;
     for (const float* p : {r->out_gamma, r->out_beta, r->in_gamma, r->in_beta, r->gate})
         if (!aligned_to(p, 4)) return UNIF_EINVAL;
-    if (r->d_model > UNIF_RESIDUAL_MAX_D) return UNIF_EUNSUPPORTED;
+    if (r->d_model < UNIF_RESIDUAL_MIN_D || r->d_model > UNIF_RESIDUAL_MAX_D) return UNIF_EUNSUPPORTED;
     return UNIF_OK;
 }
 
@@ -78,11 +78,11 @@ struct RowShape {
 };
 // 3 or 4 chunks of E columns per lane, the fewer that cover the row; rows of
 // more than one wave's 1,024 columns take a workgroup.
-RowShape row_shape(int N, int d, int cus, int waves_per_cu) {
+RowShape row_shape(int N, int d, int cus, int waves_per_cu, int narrow_threads) {
     RowShape s;
     s.lpr = 8;
     while (s.lpr < kWave && s.lpr * 4 * E < d) s.lpr *= 2;
-    s.threads = 256;
+    s.threads = narrow_threads;
     if (s.lpr * 4 * E >= d) {
         s.chunks = s.lpr * 3 * E >= d ? 3 : 4;
     } else {
@@ -92,7 +92,7 @@ RowShape row_shape(int N, int d, int cus, int waves_per_cu) {
         s.threads = (s.chunks == 3 ? w3 : w4) * kWave;
     }
     const int per_block = s.lpr == 0 ? 1 : s.threads / s.lpr;
-    const int most = std::max(1, cus * waves_per_cu / (s.threads / kWave)) * per_block;   // teams of a full chip
+    const int most = cus * std::max(1, waves_per_cu / (s.threads / kWave)) * per_block;   // teams of a full chip
     s.rows = std::max(1, ceil_div(N, most));
     s.blocks = ceil_div(ceil_div(N, s.rows), per_block);
     return s;
@@ -116,7 +116,13 @@ void with_shape(const RowShape& s, F f) {
     else with_lanes<4>(s, f);
 }
 
-constexpr int kForwardWaves = 16, kBackwardWaves = 8;   // per compute unit
+constexpr int kForwardWaves = 64, kBackwardWaves = 8;   // per compute unit
+RowShape forward_shape(const unif_moe_residual* r, int cus) {
+    return row_shape(r->n_tokens, r->d_model, cus, kForwardWaves, 256);
+}
+RowShape backward_shape(const unif_moe_residual* r, int cus) {
+    return row_shape(r->n_tokens, r->d_model, cus, kBackwardWaves, 512);
+}
 
 template <class S, class L>
 void launch_forward(const RowShape& s, const ResidualParams& p, hipStream_t st) {
@@ -161,7 +167,7 @@ struct ResidualPlan {
     size_t part, gate_part, total;
 };
 ResidualPlan plan_residual(const unif_moe_residual* r) {
-    const RowShape s = row_shape(r->n_tokens, r->d_model, kMaxCus, kBackwardWaves);
+    const RowShape s = backward_shape(r, kMaxCus);
     const size_t row = (size_t)r->d_model * sizeof(float);
     Carver cv;
     ResidualPlan p;
@@ -198,10 +204,12 @@ int32_t unif_moe_residual_forward(const unif_moe_residual* res, const void* x, c
                        Span(res->gate, gate_bytes(res))};
     if (!apart(out, partner, in)) return UNIF_EINVAL;
     if (n == 0) return UNIF_OK;
-    const RowShape sh = row_shape(res->n_tokens, res->d_model, std::min(cu_count(), kMaxCus), kForwardWaves);
+    const RowShape sh = forward_shape(res, std::min(cu_count(), kMaxCus));
     ResidualParams p = residual_params(res, sh);
     p.x = x;
     p.f = f;
+    // x is absent only beside h and so in_gamma, or beside y
+    p.spare = x != nullptr ? x : y != nullptr ? y : res->in_gamma;
     p.valid = valid;
     p.y = y;
     p.h = h;
@@ -270,7 +278,7 @@ int32_t unif_moe_residual_backward(const unif_moe_residual* res, const void* y, 
         }
         return UNIF_OK;
     }
-    const RowShape sh = row_shape(res->n_tokens, res->d_model, std::min(cu_count(), kMaxCus), kBackwardWaves);
+    const RowShape sh = backward_shape(res, std::min(cu_count(), kMaxCus));
     ResidualParams p = residual_params(res, sh);
     char* ws = align_base(workspace);
     p.grouped = gate_grouped(res);
@@ -281,6 +289,7 @@ int32_t unif_moe_residual_backward(const unif_moe_residual* res, const void* y, 
     p.dh = dh;
     p.dx = dx;
     p.df = df;
+    p.spare = ws;
     p.part = reinterpret_cast<float*>(ws + plan.part);
     p.gate_part = reinterpret_cast<float*>(ws + plan.gate_part);
     p.dgate = p.grouped ? gr.gate : nullptr;
@@ -296,10 +305,10 @@ int32_t unif_moe_residual_backward(const unif_moe_residual* res, const void* y, 
     UNIF_LAUNCH_CHECK();
     if (p.want != 0 || p.dgate != nullptr) {
         const ResidualFinish fin{p.N, p.d, sh.blocks, sh.teams(), p.group, p.rows, gate_rows(res), p.grouped, p.part,
-                                 p.gate_part, res->out_gamma, res->out_beta, res->gate, gr.out_gamma, gr.out_beta,
-                                 gr.in_gamma, gr.in_beta, gr.gate};
+                                 p.gate_part, res->out_gamma, res->out_beta, res->gate,
+                                 {gr.out_gamma, gr.out_beta, gr.in_gamma, gr.in_beta}, gr.gate};
         const int64_t shared = p.dgate != nullptr ? std::min<int64_t>(sh.teams() - 1, gate_rows(res)) : 0;
-        residual_finish_kernel<<<dim3((unsigned)ceil_div(p.d, kWave), (unsigned)(2 + shared)), kFinishWaves * kWave, 0,
+        residual_finish_kernel<<<dim3((unsigned)ceil_div(p.d, kWave), (unsigned)(4 + shared)), kFinishWaves * kWave, 0,
                                  st>>>(fin);
         UNIF_LAUNCH_CHECK();
     }

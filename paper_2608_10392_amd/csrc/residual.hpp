@@ -29,6 +29,7 @@ struct ResidualParams {
     const uint8_t* valid;
     const void* x;             // forward: x; backward: y
     const void* f;
+    const void* spare;         // d fp32 values that absent tensors' loads may read
     void* y;
     void* h;
     // backward
@@ -43,9 +44,8 @@ struct ResidualParams {
     int want;                  // bit i: partial sum i is wanted
 };
 
-// E consecutive elements of a row from column c on, E = 4; columns past d read
-// as 0. Rows start at any element, so the vector accesses assume no more than
-// the element's alignment.
+// E consecutive elements of a row, E = 4. Rows start at any element, so the
+// vector accesses assume no more than the element's alignment.
 constexpr int E = 4;
 typedef u16 u16x4 __attribute__((ext_vector_type(4)));
 typedef u16 u16x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
@@ -67,41 +67,82 @@ struct Vec<u16> {
         return __builtin_bit_cast(raw, uint2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])});
     }
 };
-template <class T>
-__device__ __forceinline__ typename Vec<T>::raw ld_raw(const T* row, int c, int d) {
-    typename Vec<T>::raw v = {};
-    if (c + E <= d) {
-        v = *reinterpret_cast<const typename Vec<T>::mem*>(row + c);
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (c + e < d) v[e] = row[c + e];
-    }
-    return v;
-}
-template <class T>
-__device__ __forceinline__ void st_cols(T* row, int c, int d, const float (&v)[E]) {
-    const typename Vec<T>::raw w = Vec<T>::pack(v);
-    if (c + E <= d) {
-        *reinterpret_cast<typename Vec<T>::mem*>(row + c) = w;
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (c + e < d) row[c + e] = w[e];
-    }
-}
 
-// A parameter row, or `other` where there is none.
-__device__ __forceinline__ void ld_param(const float* p, int c, int d, float other, float (&v)[E]) {
-    if (p != nullptr) {
-        const f32x4 w = ld_raw(p, c, d);
+#define UNIF_COLS(c, e)            \
+    _Pragma("unroll") for (int c = 0; c < CH; ++c) _Pragma("unroll") for (int e = 0; e < E; ++e)
+
+// A lane's columns: CH chunks of E, those of the row's lanes side by side.
+// Loads are issued without a branch, so that the waits for them count exactly
+// what is in flight: a chunk that reaches past the row (d >= E) reads the row's
+// last E elements instead, and fix() moves them into place, with 0 past d.
+template <int CH>
+struct Cols {
+    int d;
+    uint32_t col[CH], at[CH];   // first column, and where its load starts
+    bool full;                  // every lane's columns lie inside the row
+    __device__ __forceinline__ Cols(int d_, int lanes, int sub) : d(d_), full(d_ == CH * lanes * E) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = w[e];
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = other;
+        for (int c = 0; c < CH; ++c) {
+            col[c] = (uint32_t)(c * lanes + sub) * E;
+            at[c] = (int)col[c] + E <= d ? col[c] : (uint32_t)(d - E);
+        }
     }
-}
+    __device__ __forceinline__ bool in(int c, int e) const { return (int)col[c] + e < d; }
+    // What was loaded at at[]: in place, zeros past d and where off.
+    __device__ __forceinline__ void fix(bool on, float (&v)[CH][E]) const {
+        if (full && on) return;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const uint32_t shift = col[c] - at[c];
+            float w[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                w[e] = v[c][e];
+#pragma unroll
+                for (int k = 1; e + k < E; ++k) w[e] = shift == (uint32_t)k ? v[c][e + k] : w[e];
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[c][e] = on && in(c, e) ? w[e] : 0.f;
+        }
+    }
+    __device__ __forceinline__ void zero_past(float (&v)[CH][E]) const {
+        if (!full) UNIF_COLS(c, e) v[c][e] = in(c, e) ? v[c][e] : 0.f;
+    }
+    // The byte offset is 32 bits wide, so that rows that a wave shares are
+    // addressed from scalar registers.
+    template <class T>
+    __device__ __forceinline__ typename Vec<T>::raw load(int c, const T* row) const {
+        return *reinterpret_cast<const typename Vec<T>::mem*>(reinterpret_cast<const char*>(row) +
+                                                              at[c] * (uint32_t)sizeof(T));
+    }
+    // A parameter row, or `other` where there is none.
+    __device__ __forceinline__ void param(const float* p, float other, float (&v)[CH][E]) const {
+        if (p == nullptr) {
+            UNIF_COLS(c, e) v[c][e] = other;
+            return;
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const f32x4 w = load(c, p);
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[c][e] = w[e];
+        }
+        fix(true, v);
+    }
+    template <class T>
+    __device__ __forceinline__ void store(T* row, const float (&v)[CH][E]) const {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const typename Vec<T>::raw w = Vec<T>::pack(v[c]);
+            if ((int)col[c] + E <= d)
+                *reinterpret_cast<typename Vec<T>::mem*>(reinterpret_cast<char*>(row) + col[c] * (uint32_t)sizeof(T)) = w;
+            else
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (in(c, e)) row[col[c] + e] = w[e];
+        }
+    }
+};
 
 // v plus its value in the lane that the DPP control names.
 template <int CTRL>
@@ -142,7 +183,11 @@ struct Team {
     __device__ __forceinline__ int sub() const { return kWide ? (int)threadIdx.x : (int)threadIdx.x % kLanes; }
     __device__ __forceinline__ int local() const { return kWide ? 0 : (int)threadIdx.x / kLanes; }
     __device__ __forceinline__ int index() const {
-        return kWide ? (int)blockIdx.x : (int)((blockIdx.x * blockDim.x + threadIdx.x) / kLanes);
+        // a whole wave's number is scalar, and so are its rows' addresses
+        if constexpr (kWide) return (int)blockIdx.x;
+        else if constexpr (kLanes == kWave)
+            return (int)(blockIdx.x * (blockDim.x / kWave)) + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+        else return (int)((blockIdx.x * blockDim.x + threadIdx.x) / kLanes);
     }
     template <int NV>
     __device__ __forceinline__ void sum(float (&v)[NV]) {
@@ -165,20 +210,53 @@ struct Team {
     }
 };
 
-#define UNIF_COLS(c, e)            \
-    _Pragma("unroll") for (int c = 0; c < CH; ++c) _Pragma("unroll") for (int e = 0; e < E; ++e)
-
+// One row of a tensor on its way. Rows that are not wanted (padded tokens, the
+// row past a team's last) and tensors that are absent are loaded from a row that
+// is there and read as zeros.
 template <class T, int CH>
 struct RowRaw {
+    const T* base;
+    int64_t stride;   // 0: absent
+    bool on;
     typename Vec<T>::raw v[CH];
-    __device__ __forceinline__ void load(const void* p, size_t at, const int (&col)[CH], int d, bool on) {
+    __device__ __forceinline__ RowRaw(const void* p, const void* other, int d)
+        : base(static_cast<const T*>(p != nullptr ? p : other)), stride(p != nullptr ? d : 0), on(false) {}
+    __device__ __forceinline__ void load(const Cols<CH>& k, int64_t r, bool real) {
+        on = real && stride != 0;
+        const T* const row = base + r * stride;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            if (on && p != nullptr) v[c] = ld_raw(static_cast<const T*>(p) + at, col[c], d);
-            else v[c] = typename Vec<T>::raw{};
-        }
+        for (int c = 0; c < CH; ++c) v[c] = k.load(c, row);
     }
-    __device__ __forceinline__ void get(float (&u)[CH][E]) const { UNIF_COLS(c, e) u[c][e] = Vec<T>::get(v[c], e); }
+    __device__ __forceinline__ void get(const Cols<CH>& k, float (&u)[CH][E]) const {
+        UNIF_COLS(c, e) u[c][e] = Vec<T>::get(v[c], e);
+        k.fix(on, u);
+    }
+};
+
+// Which of a team's tokens are real, 64 at a time: the lanes read their flags
+// side by side.
+template <int LANES>
+struct RealRows {
+    const uint8_t* valid;
+    int64_t r0, r1;
+    uint64_t bits;
+    __device__ __forceinline__ RealRows(const uint8_t* v, int64_t r0_, int64_t r1_) : valid(v), r0(r0_), r1(r1_), bits(0) {}
+    // Rows are asked for in order, from r0 on.
+    __device__ __forceinline__ bool operator()(int64_t r) {
+        if (valid == nullptr) return r < r1;
+        const int i = (int)((r - r0) & 63);
+        if (i == 0) {
+            const int lane = lane_id(), sub = lane % LANES, first = lane - sub;
+            bits = 0;
+#pragma unroll
+            for (int k = 0; k < kWave / LANES; ++k) {
+                const int64_t t = r + k * LANES + sub;
+                const uint64_t b = ballot(t < r1 && valid[t] != 0) >> first;
+                bits |= (LANES == kWave ? b : b & ((1ull << (LANES & 63)) - 1)) << (k * LANES & 63);
+            }
+        }
+        return bits >> i & 1;
+    }
 };
 
 template <int CH>
@@ -194,18 +272,19 @@ __device__ __forceinline__ float row_dot(const float (&a)[CH][E], const float (&
     return s;
 }
 template <int CH>
-__device__ __forceinline__ void centre(float mean, int d, const int (&col)[CH], float (&u)[CH][E]) {
-    UNIF_COLS(c, e) u[c][e] = col[c] + e < d ? u[c][e] - mean : 0.f;   // columns past d stay out of the sums
+__device__ __forceinline__ void centre(const Cols<CH>& k, float mean, float (&u)[CH][E]) {
+    UNIF_COLS(c, e) u[c][e] -= mean;
+    k.zero_past(u);   // columns past d stay out of the sums
 }
 
 // Replaces the row u by its normalised values.
 template <int CH, int LPR>
-__device__ __forceinline__ void normalise(Team<LPR>& team, int norm, float eps, float inv_d, int d,
-                                          const int (&col)[CH], float (&u)[CH][E]) {
+__device__ __forceinline__ void normalise(Team<LPR>& team, const Cols<CH>& k, int norm, float eps, float inv_d,
+                                          float (&u)[CH][E]) {
     if (norm == kNormLayer) {
         float s[1] = {row_sum<CH>(u)};
         team.sum(s);
-        centre<CH>(s[0] * inv_d, d, col, u);
+        centre<CH>(k, s[0] * inv_d, u);
     }
     float q[1] = {row_dot<CH>(u, u)};
     team.sum(q);
@@ -218,72 +297,60 @@ __device__ __forceinline__ void normalise(Team<LPR>& team, int norm, float eps, 
 template <int CH, int LPR>
 __device__ __forceinline__ void normalise_grad(Team<LPR>& team, int norm, float rstd, float inv_d,
                                                const float (&hat)[CH][E], float (&a)[CH][E]) {
-    float s[2] = {row_sum<CH>(a), row_dot<CH>(a, hat)};
+    float s[2] = {0.f, row_dot<CH>(a, hat)};
+    if (norm == kNormLayer) s[0] = row_sum<CH>(a);
     team.sum(s);
-    const float m = norm == kNormLayer ? s[0] * inv_d : 0.f, q = s[1] * inv_d;
-    UNIF_COLS(c, e) a[c][e] = rstd * (fmaf(-hat[c][e], q, a[c][e]) - m);
+    const float m = -rstd * inv_d * s[0], q = -rstd * inv_d * s[1];
+    UNIF_COLS(c, e) a[c][e] = fmaf(hat[c][e], q, fmaf(a[c][e], rstd, m));
 }
 
 template <class S, class L, int CH, int LPR>
 __global__ __launch_bounds__(LPR == 0 ? 512 : 256) void residual_forward_kernel(ResidualParams p) {
     __shared__ float red[2 * kWideWaves * 4];
     Team<LPR> team{red, 0};
-    int col[CH];
-#pragma unroll
-    for (int c = 0; c < CH; ++c) col[c] = (c * team.size() + team.sub()) * E;
+    const Cols<CH> k(p.d, team.size(), team.sub());
     const int64_t r0 = (int64_t)team.index() * p.rows;
     const int64_t r1 = r0 + p.rows < p.N ? r0 + p.rows : p.N;
     if (r0 >= r1) return;
-    auto is_real = [&](int64_t r) { return r < r1 && (p.valid == nullptr || p.valid[r] != 0); };
-    RowRaw<S, CH> xr;
-    RowRaw<L, CH> fr;
-    bool real = is_real(r0), next = is_real(r0 + 1);
-    xr.load(p.x, (size_t)r0 * p.d, col, p.d, real);
-    fr.load(p.f, (size_t)r0 * p.d, col, p.d, real);
+    RealRows<Team<LPR>::kLanes> is_real(p.valid, r0, r1);
+    RowRaw<S, CH> x(p.x, p.spare, p.d);
+    RowRaw<L, CH> f(p.f, p.spare, p.d);
+    bool real = is_real(r0);
+    x.load(k, r0, real);
+    f.load(k, r0, real);
     // v = s x + cg f_hat + cb with cg = gate gamma_out, cb = gate beta_out
     float cg[CH][E], cb[CH][E], ig[CH][E], ib[CH][E];
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        ld_param(p.in_gamma, col[c], p.d, 1.f, ig[c]);
-        ld_param(p.in_beta, col[c], p.d, 0.f, ib[c]);
-    }
+    k.param(p.in_gamma, 1.f, ig);
+    k.param(p.in_beta, 0.f, ib);
     int64_t gend = r0;   // cg and cb serve the tokens before gend
     for (int64_t r = r0; r < r1; ++r) {
         if (r >= gend) {
             const int64_t g = r / p.group;
             gend = (g + 1) * p.group;
-#pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                float gt[E];
-                ld_param(p.gate == nullptr ? nullptr : p.gate + g * p.d, col[c], p.d, 1.f, gt);
-                ld_param(p.out_gamma, col[c], p.d, 1.f, cg[c]);
-                ld_param(p.out_beta, col[c], p.d, 0.f, cb[c]);
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    cg[c][e] *= gt[e];
-                    cb[c][e] *= gt[e];
-                }
-            }
+            float gt[CH][E];
+            k.param(p.gate == nullptr ? nullptr : p.gate + g * p.d, 1.f, gt);
+            k.param(p.out_gamma, 1.f, cg);
+            k.param(p.out_beta, 0.f, cb);
+            UNIF_COLS(c, e) cg[c][e] *= gt[c][e];
+            UNIF_COLS(c, e) cb[c][e] *= gt[c][e];
         }
         const size_t at = (size_t)r * p.d;
-        float v[CH][E], x[CH][E];
-        fr.get(v);
-        xr.get(x);
+        float v[CH][E], u[CH][E];
+        f.get(k, v);
+        x.get(k, u);
         const bool keep = real;
-        real = next;
-        next = is_real(r + 2);
-        xr.load(p.x, at + p.d, col, p.d, real);
-        fr.load(p.f, at + p.d, col, p.d, real);
-        if (p.out_norm != kNormNone) normalise<CH, LPR>(team, p.out_norm, p.out_eps, p.inv_d, p.d, col, v);
-        UNIF_COLS(c, e) v[c][e] = keep ? fmaf(p.scale, x[c][e], fmaf(v[c][e], cg[c][e], cb[c][e])) : 0.f;
-        if (p.y != nullptr)
-#pragma unroll
-            for (int c = 0; c < CH; ++c) st_cols(static_cast<S*>(p.y) + at, col[c], p.d, v[c]);
+        real = is_real(r + 1);
+        x.load(k, real ? r + 1 : r, real);
+        f.load(k, real ? r + 1 : r, real);
+        if (p.out_norm != kNormNone) normalise<CH, LPR>(team, k, p.out_norm, p.out_eps, p.inv_d, v);
+        UNIF_COLS(c, e) v[c][e] = fmaf(p.scale, u[c][e], fmaf(v[c][e], cg[c][e], cb[c][e]));
+        if (!keep) UNIF_COLS(c, e) v[c][e] = 0.f;
+        if (p.y != nullptr) k.store(static_cast<S*>(p.y) + at, v);
         if (p.h != nullptr) {
-            normalise<CH, LPR>(team, p.in_norm, p.in_eps, p.inv_d, p.d, col, v);
-            UNIF_COLS(c, e) v[c][e] = keep ? fmaf(v[c][e], ig[c][e], ib[c][e]) : 0.f;
-#pragma unroll
-            for (int c = 0; c < CH; ++c) st_cols(static_cast<L*>(p.h) + at, col[c], p.d, v[c]);
+            normalise<CH, LPR>(team, k, p.in_norm, p.in_eps, p.inv_d, v);
+            UNIF_COLS(c, e) v[c][e] = fmaf(v[c][e], ig[c][e], ib[c][e]);
+            if (!keep) UNIF_COLS(c, e) v[c][e] = 0.f;
+            k.store(static_cast<L*>(p.h) + at, v);
         }
     }
 }
@@ -303,101 +370,86 @@ __global__ __launch_bounds__(LPR == 0 ? 512 : 256) void residual_forward_kernel(
 constexpr int kSumOutGamma = 0, kSumOutBeta = 1, kSumInGamma = 2, kSumInBeta = 3;
 
 template <class S, class L, class H, int CH, int LPR>
-__global__ __launch_bounds__(LPR == 0 ? 512 : 256) void residual_backward_kernel(ResidualParams p) {
+__global__ __launch_bounds__(512) void residual_backward_kernel(ResidualParams p) {
     __shared__ float red[2 * kWideWaves * 4];
     extern __shared__ float sums[];   // [teams of the workgroup][2][d]
     Team<LPR> team{red, 0};
-    int col[CH];
-#pragma unroll
-    for (int c = 0; c < CH; ++c) col[c] = (c * team.size() + team.sub()) * E;
+    const Cols<CH> k(p.d, team.size(), team.sub());
     float* const mine = sums + (size_t)team.local() * 2 * p.d;
     const int64_t r0 = (int64_t)team.index() * p.rows;
     const int64_t r1 = r0 + p.rows < p.N ? r0 + p.rows : p.N;
-    auto is_real = [&](int64_t r) { return r < r1 && (p.valid == nullptr || p.valid[r] != 0); };
-    RowRaw<S, CH> yr, gr;
-    RowRaw<H, CH> hr;
-    RowRaw<L, CH> fr;
-    bool real = is_real(r0), next = is_real(r0 + 1);
-    yr.load(p.x, (size_t)r0 * p.d, col, p.d, real);
-    fr.load(p.f, (size_t)r0 * p.d, col, p.d, real);
-    hr.load(p.dh, (size_t)r0 * p.d, col, p.d, real);
-    gr.load(p.dy, (size_t)r0 * p.d, col, p.d, real);
+    RealRows<Team<LPR>::kLanes> is_real(p.valid, r0, r1);
+    RowRaw<S, CH> yr(p.x, p.spare, p.d), gr(p.dy, p.spare, p.d);
+    RowRaw<H, CH> hr(p.dh, p.spare, p.d);
+    RowRaw<L, CH> fr(p.f, p.spare, p.d);
+    bool real = is_real(r0);
+    const int64_t start = r0 < p.N ? r0 : 0;
+    yr.load(k, start, real);
+    fr.load(k, start, real);
+    hr.load(k, start, real);
+    gr.load(k, start, real);
     float acc[4][CH][E];
 #pragma unroll
     for (int i = 0; i < 4; ++i) UNIF_COLS(c, e) acc[i][c][e] = 0.f;
     if (p.grouped) {
-        const float zero[E] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            st_cols(mine, col[c], p.d, zero);
-            st_cols(mine + p.d, col[c], p.d, zero);
-        }
+        k.store(mine, acc[kSumOutGamma]);
+        k.store(mine + p.d, acc[kSumOutBeta]);
     }
     float ig[CH][E], cg[CH][E];   // cg = gate gamma_out
-#pragma unroll
-    for (int c = 0; c < CH; ++c) ld_param(p.in_gamma, col[c], p.d, 1.f, ig[c]);
+    k.param(p.in_gamma, 1.f, ig);
     int64_t g = -1, gend = r0;
     auto flush = [&]() {
         const int64_t g0 = g * p.group, g1 = gend < p.N ? gend : p.N;
         float* const dst = (g0 >= r0 && g1 <= r1) ? p.dgate + g * p.d
                                                   : p.gate_part + ((size_t)team.index() * 2 + (g0 > r0 ? 1 : 0)) * p.d;
+        float w[CH][E], v[CH][E];
+        if (p.dgate != nullptr) {
+            k.param(p.out_gamma, 1.f, w);
+            k.param(p.out_beta, 0.f, v);
+            UNIF_COLS(c, e) w[c][e] = fmaf(w[c][e], acc[kSumOutGamma][c][e], v[c][e] * acc[kSumOutBeta][c][e]);
+            k.store(dst, w);
+        }
+        k.param(p.gate + g * p.d, 1.f, w);
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            float og[E], ob[E], gt[E], t0[E], t1[E], dg[E];
-            ld_param(p.out_gamma, col[c], p.d, 1.f, og);
-            ld_param(p.out_beta, col[c], p.d, 0.f, ob);
-            ld_param(p.gate + g * p.d, col[c], p.d, 1.f, gt);
-            ld_param(mine, col[c], p.d, 0.f, t0);
-            ld_param(mine + p.d, col[c], p.d, 0.f, t1);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                dg[e] = fmaf(og[e], acc[kSumOutGamma][c][e], ob[e] * acc[kSumOutBeta][c][e]);
-                t0[e] = fmaf(gt[e], acc[kSumOutGamma][c][e], t0[e]);
-                t1[e] = fmaf(gt[e], acc[kSumOutBeta][c][e], t1[e]);
-                acc[kSumOutGamma][c][e] = acc[kSumOutBeta][c][e] = 0.f;
-            }
-            if (p.dgate != nullptr) st_cols(dst, col[c], p.d, dg);
-            st_cols(mine, col[c], p.d, t0);
-            st_cols(mine + p.d, col[c], p.d, t1);
+        for (int i = 0; i < 2; ++i) {
+            k.param(mine + i * p.d, 0.f, v);
+            UNIF_COLS(c, e) v[c][e] = fmaf(w[c][e], acc[i][c][e], v[c][e]);
+            k.store(mine + i * p.d, v);
+            UNIF_COLS(c, e) acc[i][c][e] = 0.f;
         }
     };
-    const float mask_in = p.in_norm == kNormLayer ? p.inv_d : 0.f, mask_out = p.out_norm == kNormLayer ? p.inv_d : 0.f;
     for (int64_t r = r0; r < r1; ++r) {
         if (r >= gend) {
             if (p.grouped && g >= 0) flush();
             g = r / p.group;
             gend = (g + 1) * p.group;
-#pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                float gt[E];
-                ld_param(p.gate == nullptr ? nullptr : p.gate + g * p.d, col[c], p.d, 1.f, gt);
-                ld_param(p.out_gamma, col[c], p.d, 1.f, cg[c]);
-#pragma unroll
-                for (int e = 0; e < E; ++e) cg[c][e] *= gt[e];
-            }
+            float gt[CH][E];
+            k.param(p.gate == nullptr ? nullptr : p.gate + g * p.d, 1.f, gt);
+            k.param(p.out_gamma, 1.f, cg);
+            UNIF_COLS(c, e) cg[c][e] *= gt[c][e];
         }
         // Each tensor's next row is loaded as soon as this one's is in use.
         const size_t at = (size_t)r * p.d;
         float y[CH][E], D[CH][E], f[CH][E];
-        yr.get(y);
-        fr.get(f);
-        real = next;
-        next = is_real(r + 2);
-        yr.load(p.x, at + p.d, col, p.d, real);
-        fr.load(p.f, at + p.d, col, p.d, real);
+        yr.get(k, y);
+        fr.get(k, f);
+        real = is_real(r + 1);
+        const int64_t ahead = real ? r + 1 : r;
+        yr.load(k, ahead, real);
+        fr.load(k, ahead, real);
         // both norms' statistics side by side: means, then squares
         if (p.in_norm == kNormLayer || p.out_norm == kNormLayer) {
             float s[2] = {row_sum<CH>(y), row_sum<CH>(f)};
             team.sum(s);
-            if (p.in_norm == kNormLayer) centre<CH>(s[0] * mask_in, p.d, col, y);
-            if (p.out_norm == kNormLayer) centre<CH>(s[1] * mask_out, p.d, col, f);
+            if (p.in_norm == kNormLayer) centre<CH>(k, s[0] * p.inv_d, y);
+            if (p.out_norm == kNormLayer) centre<CH>(k, s[1] * p.inv_d, f);
         }
         float q[2] = {row_dot<CH>(y, y), row_dot<CH>(f, f)};
         team.sum(q);
         const float r_in = rsqrtf(fmaf(q[0], p.inv_d, p.in_eps));
         const float r_out = p.out_norm == kNormNone ? 1.f : rsqrtf(fmaf(q[1], p.inv_d, p.out_eps));
-        hr.get(D);
-        hr.load(p.dh, at + p.d, col, p.d, real);
+        hr.get(k, D);
+        hr.load(k, ahead, real);
         if (p.dh != nullptr) {
             UNIF_COLS(c, e) {
                 y[c][e] *= r_in;
@@ -407,16 +459,14 @@ __global__ __launch_bounds__(LPR == 0 ? 512 : 256) void residual_backward_kernel
             }
             normalise_grad<CH, LPR>(team, p.in_norm, r_in, p.inv_d, y, D);
         }
-        UNIF_COLS(c, e) D[c][e] += Vec<S>::get(gr.v[c], e);
-        gr.load(p.dy, at + p.d, col, p.d, real);
-        if (p.dx != nullptr)
-#pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                float o[E];
-#pragma unroll
-                for (int e = 0; e < E; ++e) o[e] = p.scale * D[c][e];
-                st_cols(static_cast<S*>(p.dx) + at, col[c], p.d, o);
-            }
+        float dy[CH][E];
+        gr.get(k, dy);
+        gr.load(k, ahead, real);
+        UNIF_COLS(c, e) D[c][e] += dy[c][e];
+        if (p.dx != nullptr) {
+            UNIF_COLS(c, e) dy[c][e] = p.scale * D[c][e];
+            k.store(static_cast<S*>(p.dx) + at, dy);
+        }
         UNIF_COLS(c, e) {
             f[c][e] *= r_out;
             acc[kSumOutGamma][c][e] = fmaf(D[c][e], f[c][e], acc[kSumOutGamma][c][e]);
@@ -425,39 +475,32 @@ __global__ __launch_bounds__(LPR == 0 ? 512 : 256) void residual_backward_kernel
         }
         if (p.df != nullptr) {
             if (p.out_norm != kNormNone) normalise_grad<CH, LPR>(team, p.out_norm, r_out, p.inv_d, f, D);
-#pragma unroll
-            for (int c = 0; c < CH; ++c) st_cols(static_cast<L*>(p.df) + at, col[c], p.d, D[c]);
+            k.store(static_cast<L*>(p.df) + at, D);
         }
     }
     if (p.want == 0 && p.dgate == nullptr) return;
     if (p.grouped) {
         if (g >= 0) flush();
     } else {
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            st_cols(mine, col[c], p.d, acc[kSumOutGamma][c]);
-            st_cols(mine + p.d, col[c], p.d, acc[kSumOutBeta][c]);
-        }
+        k.store(mine, acc[kSumOutGamma]);
+        k.store(mine + p.d, acc[kSumOutBeta]);
     }
     // The teams' sums in team order, one partial row each per workgroup.
     const int nteam = (int)blockDim.x / team.size();
     auto add_teams = [&](int first) {
         __syncthreads();
         for (int i = threadIdx.x; i < 2 * p.d; i += blockDim.x) {
-            const int k = first + (i >= p.d ? 1 : 0);
-            if (!(p.want >> k & 1)) continue;
+            const int which = first + (i >= p.d ? 1 : 0);
+            if (!(p.want >> which & 1)) continue;
             float s = 0.f;
             for (int t = 0; t < nteam; ++t) s += sums[(size_t)t * 2 * p.d + i];
-            p.part[((size_t)k * gridDim.x + blockIdx.x) * p.d + (i >= p.d ? i - p.d : i)] = s;
+            p.part[((size_t)which * gridDim.x + blockIdx.x) * p.d + (i >= p.d ? i - p.d : i)] = s;
         }
     };
     add_teams(kSumOutGamma);
     __syncthreads();
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        st_cols(mine, col[c], p.d, acc[kSumInGamma][c]);
-        st_cols(mine + p.d, col[c], p.d, acc[kSumInBeta][c]);
-    }
+    k.store(mine, acc[kSumInGamma]);
+    k.store(mine + p.d, acc[kSumInBeta]);
     add_teams(kSumInGamma);
 }
 
@@ -470,19 +513,16 @@ struct ResidualFinish {
     const float* out_gamma;
     const float* out_beta;
     const float* gate;
-    float* d_out_gamma;      // NULL: not wanted
-    float* d_out_beta;
-    float* d_in_gamma;
-    float* d_in_beta;
+    float* d_sum[4];         // gradients of the parameters by their sum (NULL: not wanted)
     float* d_gate;
 };
 
 // 64 columns per workgroup, the waves a stretch of the partial rows each, the
-// stretches added in order, all in fp64. blockIdx.y 0 and 1: the sums of D
-// f_hat and D (and with one gate row its gradient, in 0) and of dh v_hat and
-// dh; from 2 on: gate rows whose tokens several teams share. Those are found
-// from the ends of the teams' tokens, or, where there are fewer, from the gate
-// rows: a row belongs to the first team's end that lies inside it.
+// stretches added in order, all in fp64. blockIdx.y 0 to 3: the sums (0 also
+// forms the gradient of a single gate row, from two of them); from 4 on: gate
+// rows whose tokens several teams share. Those are found from the ends of the
+// teams' tokens, or, where there are fewer, from the gate rows: a row belongs to
+// the first team's end that lies inside it.
 constexpr int kFinishWaves = 16;
 
 __global__ __launch_bounds__(kFinishWaves* kWave) void residual_finish_kernel(ResidualFinish p) {
@@ -508,31 +548,26 @@ __global__ __launch_bounds__(kFinishWaves* kWave) void residual_finish_kernel(Re
         for (int k = 0; k < kFinishWaves; ++k) s += stretch[i][k][lane];
         return s;
     };
-    if (blockIdx.y < 2) {
-        const float* const src = p.part + (size_t)blockIdx.y * 2 * p.parts * p.d + n;
-        const bool a = blockIdx.y == 1 ? p.d_in_gamma != nullptr : p.d_out_gamma != nullptr || (!p.grouped && p.d_gate != nullptr);
-        const bool b = blockIdx.y == 1 ? p.d_in_beta != nullptr : p.d_out_beta != nullptr || (!p.grouped && p.d_gate != nullptr);
-        stretch[0][w][lane] = (a && n < p.d) ? column(src, p.parts, p.d) : 0.0;
-        stretch[1][w][lane] = (b && n < p.d) ? column(src + (size_t)p.parts * p.d, p.parts, p.d) : 0.0;
+    if (blockIdx.y < 4) {
+        const int i = (int)blockIdx.y;
+        const bool gate = i == kSumOutGamma && !p.grouped && p.d_gate != nullptr;
+        float* const out = p.d_sum[i];
+        if (out == nullptr && !gate) return;
+        const float* const src = p.part + (size_t)i * p.parts * p.d + n;
+        stretch[0][w][lane] = n < p.d ? column(src, p.parts, p.d) : 0.0;
+        stretch[1][w][lane] = gate && n < p.d ? column(src + (size_t)p.parts * p.d, p.parts, p.d) : 0.0;
         __syncthreads();
         if (w != 0 || n >= p.d) return;
-        const double s0 = total(0), s1 = total(1);
-        if (blockIdx.y == 1) {
-            if (p.d_in_gamma != nullptr) p.d_in_gamma[n] = (float)s0;
-            if (p.d_in_beta != nullptr) p.d_in_beta[n] = (float)s1;
-            return;
-        }
-        const double gt = (!p.grouped && p.gate != nullptr) ? (double)p.gate[n] : 1.0;
-        if (p.d_out_gamma != nullptr) p.d_out_gamma[n] = (float)(gt * s0);
-        if (p.d_out_beta != nullptr) p.d_out_beta[n] = (float)(gt * s1);
-        if (!p.grouped && p.d_gate != nullptr)
-            p.d_gate[n] = (float)((p.out_gamma != nullptr ? (double)p.out_gamma[n] : 1.0) * s0 +
-                                  (p.out_beta != nullptr ? (double)p.out_beta[n] * s1 : 0.0));
+        const double s = total(0);
+        if (out != nullptr) out[n] = (float)(i <= kSumOutBeta && !p.grouped && p.gate != nullptr ? s * (double)p.gate[n] : s);
+        if (gate)
+            p.d_gate[n] = (float)((p.out_gamma != nullptr ? (double)p.out_gamma[n] : 1.0) * s +
+                                  (p.out_beta != nullptr ? (double)p.out_beta[n] * total(1) : 0.0));
         return;
     }
-    int64_t g = (int64_t)blockIdx.y - 2;
+    int64_t g = (int64_t)blockIdx.y - 4;
     if (p.teams - 1 < p.groups) {
-        const int64_t end = (g + 1) * p.rows;   // of team blockIdx.y - 2
+        const int64_t end = (g + 1) * p.rows;   // of team blockIdx.y - 4
         g = end / p.group;
         if (end >= p.N || g * p.group == end || end - p.rows > g * p.group) return;
     }

@@ -195,7 +195,7 @@ def check_both(c, label):
         check(k, v, *want[k])
 
 
-WIDTHS = [1, 7, 8, 63, 64, 65, 128, 200, 256, 257, 384, 512, 513, 768, 1000, 1024, 1025, 1536, 2048, 4096, 5120, 8191,
+WIDTHS = [4, 5, 6, 7, 8, 63, 64, 65, 128, 200, 256, 257, 384, 512, 513, 768, 1000, 1024, 1025, 1536, 2048, 4096, 5120, 8191,
           8192]
 
 

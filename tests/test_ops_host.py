@@ -91,7 +91,9 @@ def test_bad_descriptions_are_rejected(L, bad):
     assert backward(L, r) == _lib.EINVAL
 
 
-def test_wide_rows_are_unsupported(L):
+def test_rows_out_of_range_are_unsupported(L):
+    assert forward(L, residual(d_model=ops.RESIDUAL_MIN_D - 1)) == _lib.EUNSUPPORTED
+    assert backward(L, residual(d_model=ops.RESIDUAL_MIN_D - 1)) == _lib.EUNSUPPORTED
     assert forward(L, residual(d_model=ops.RESIDUAL_MAX_D + 1)) == _lib.EUNSUPPORTED
     assert backward(L, residual(d_model=ops.RESIDUAL_MAX_D + 1)) == _lib.EUNSUPPORTED
     assert ops.residual_backward_workspace_size(residual(d_model=ops.RESIDUAL_MAX_D)) > 0
