@@ -76,30 +76,33 @@ struct RowShape {
     int lpr, chunks, threads, rows, blocks;
     int teams() const { return lpr == 0 ? blocks : blocks * (threads / lpr); }
 };
-// 3 or 4 chunks of E columns per lane, the fewer that cover the row; rows of
-// more than one wave's 1,024 columns take a workgroup.
-RowShape row_shape(int N, int d, int cus, int waves_per_cu, int narrow_threads) {
-    RowShape s;
+// Rows of up to 1,024 columns are a part of a wave's, 3 or 4 chunks of E columns
+// per lane, the fewer that cover the row; wider ones take a workgroup.
+RowShape narrow_shape(int d, int threads) {
+    RowShape s{};
     s.lpr = 8;
     while (s.lpr < kWave && s.lpr * 4 * E < d) s.lpr *= 2;
-    s.threads = narrow_threads;
-    if (s.lpr * 4 * E >= d) {
-        s.chunks = s.lpr * 3 * E >= d ? 3 : 4;
-    } else {
-        s.lpr = 0;
-        const int w3 = ceil_div(d, kWave * 3 * E), w4 = ceil_div(d, kWave * 4 * E);
-        s.chunks = w3 * 3 < w4 * 4 && w3 <= kWideWaves ? 3 : 4;
-        s.threads = (s.chunks == 3 ? w3 : w4) * kWave;
-    }
+    s.chunks = s.lpr * 3 * E >= d ? 3 : 4;
+    s.threads = threads;
+    return s;
+}
+RowShape wide_shape(int d, int chunks) {
+    RowShape s{};
+    s.chunks = chunks;
+    s.threads = ceil_div(d, kWave * chunks * E) * kWave;
+    return s;
+}
+// The tokens dealt to at most `waves` waves per compute unit.
+RowShape cover(RowShape s, int N, int cus, int waves) {
     const int per_block = s.lpr == 0 ? 1 : s.threads / s.lpr;
-    const int most = cus * std::max(1, waves_per_cu / (s.threads / kWave)) * per_block;   // teams of a full chip
+    const int most = cus * std::max(1, waves / (s.threads / kWave)) * per_block;
     s.rows = std::max(1, ceil_div(N, most));
     s.blocks = ceil_div(ceil_div(N, s.rows), per_block);
     return s;
 }
 
 // Calls f(chunks, lanes per row) for a launch's shape.
-template <int CH, class F>
+template <int CH, int Wide, class F>
 void with_lanes(const RowShape& s, F f) {
     const std::integral_constant<int, CH> ch;
     switch (s.lpr) {
@@ -107,36 +110,46 @@ void with_lanes(const RowShape& s, F f) {
         case 16: return f(ch, std::integral_constant<int, 16>());
         case 32: return f(ch, std::integral_constant<int, 32>());
         case 64: return f(ch, std::integral_constant<int, 64>());
-        default: return f(ch, std::integral_constant<int, 0>());
+        default: return f(std::integral_constant<int, Wide>(), std::integral_constant<int, 0>());
     }
 }
-template <class F>
-void with_shape(const RowShape& s, F f) {
-    if (s.chunks == 3) with_lanes<3>(s, f);
-    else with_lanes<4>(s, f);
-}
 
-constexpr int kForwardWaves = 64, kBackwardWaves = 8;   // per compute unit
+constexpr int kNarrowD = kWave * 4 * E;
+// Forward: many more waves than run at once, so that the last ones of a launch
+// leave little of the chip idle, but fewer where a wave holds several rows and
+// the parameters' loads would weigh: 65,536 x 1,024 bf16 113.5 us with 16 waves
+// per compute unit, 111 with 32, 108.8 with 64; 200,000 x 128 46 with 16, 51 with
+// 32, 52 with 64. Wide rows in 2 chunks a lane: 16,384 x 2,048 66.6 us, in 4 77.
 RowShape forward_shape(const unif_moe_residual* r, int cus) {
-    return row_shape(r->n_tokens, r->d_model, cus, kForwardWaves, 256);
+    if (r->d_model > kNarrowD) return cover(wide_shape(r->d_model, 2), r->n_tokens, cus, 32);
+    const RowShape s = narrow_shape(r->d_model, 256);
+    return cover(s, r->n_tokens, cus, std::max(16, s.lpr));
 }
+// Backward: as many waves as run at once (two per SIMD, by their registers), so
+// that the partial rows are few: 50,432 x 768 134 us with 8 waves per compute
+// unit, 168 with 4, 158 with 24. Wide rows in 4 chunks a lane: 16,384 x 4,096
+// 183 us, in 3 247, in 2 226 to 283.
 RowShape backward_shape(const unif_moe_residual* r, int cus) {
-    return row_shape(r->n_tokens, r->d_model, cus, kBackwardWaves, 512);
+    return cover(r->d_model > kNarrowD ? wide_shape(r->d_model, 4) : narrow_shape(r->d_model, 512), r->n_tokens, cus, 8);
 }
 
 template <class S, class L>
 void launch_forward(const RowShape& s, const ResidualParams& p, hipStream_t st) {
-    with_shape(s, [&](auto ch, auto lpr) {
+    const auto launch = [&](auto ch, auto lpr) {
         residual_forward_kernel<S, L, ch.value, lpr.value><<<(unsigned)s.blocks, (unsigned)s.threads, 0, st>>>(p);
-    });
+    };
+    if (s.chunks == 3) with_lanes<3, 2>(s, launch);
+    else with_lanes<4, 2>(s, launch);
 }
 template <class S, class L, class H>
 void launch_backward(const RowShape& s, const ResidualParams& p, hipStream_t st) {
     const size_t lds = (size_t)(s.teams() / s.blocks) * 2 * p.d * sizeof(float);
-    with_shape(s, [&](auto ch, auto lpr) {
+    const auto launch = [&](auto ch, auto lpr) {
         residual_backward_kernel<S, L, H, ch.value, lpr.value>
             <<<(unsigned)s.blocks, (unsigned)s.threads, lds, st>>>(p);
-    });
+    };
+    if (s.chunks == 3) with_lanes<3, 4>(s, launch);
+    else with_lanes<4, 4>(s, launch);
 }
 
 ResidualParams residual_params(const unif_moe_residual* r, const RowShape& s) {
@@ -304,10 +317,12 @@ int32_t unif_moe_residual_backward(const unif_moe_residual* res, const void* y, 
     else launch_backward<u16, u16, u16>(sh, p, st);
     UNIF_LAUNCH_CHECK();
     if (p.want != 0 || p.dgate != nullptr) {
-        const ResidualFinish fin{p.N, p.d, sh.blocks, sh.teams(), p.group, p.rows, gate_rows(res), p.grouped, p.part,
+        const int by_wave = p.group / p.rows <= kFinishWaves;
+        const ResidualFinish fin{p.N, p.d, sh.blocks, sh.teams(), p.group, p.rows, gate_rows(res), by_wave, p.grouped, p.part,
                                  p.gate_part, res->out_gamma, res->out_beta, res->gate,
                                  {gr.out_gamma, gr.out_beta, gr.in_gamma, gr.in_beta}, gr.gate};
-        const int64_t shared = p.dgate != nullptr ? std::min<int64_t>(sh.teams() - 1, gate_rows(res)) : 0;
+        int64_t shared = p.dgate != nullptr ? std::min<int64_t>(sh.teams() - 1, gate_rows(res)) : 0;
+        if (by_wave) shared = (shared + kFinishWaves - 1) / kFinishWaves;
         residual_finish_kernel<<<dim3((unsigned)ceil_div(p.d, kWave), (unsigned)(4 + shared)), kFinishWaves * kWave, 0,
                                  st>>>(fin);
         UNIF_LAUNCH_CHECK();

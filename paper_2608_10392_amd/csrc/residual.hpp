@@ -172,7 +172,7 @@ __device__ __forceinline__ float lanes_sum(float v) {
 
 // The lanes that hold one row: LPR lanes of a wave, or (LPR = 0) all waves of
 // the workgroup, whose sums are added in order.
-constexpr int kWideWaves = 8;   // most waves of a wide team
+constexpr int kWideWaves = 16;   // most waves of a wide team (backward: 8)
 template <int LPR>
 struct Team {
     static constexpr bool kWide = LPR == 0;
@@ -305,7 +305,7 @@ __device__ __forceinline__ void normalise_grad(Team<LPR>& team, int norm, float 
 }
 
 template <class S, class L, int CH, int LPR>
-__global__ __launch_bounds__(LPR == 0 ? 512 : 256) void residual_forward_kernel(ResidualParams p) {
+__global__ __launch_bounds__(LPR == 0 ? kWideWaves * kWave : 256) void residual_forward_kernel(ResidualParams p) {
     __shared__ float red[2 * kWideWaves * 4];
     Team<LPR> team{red, 0};
     const Cols<CH> k(p.d, team.size(), team.sub());
@@ -507,6 +507,7 @@ __global__ __launch_bounds__(512) void residual_backward_kernel(ResidualParams p
 struct ResidualFinish {
     int N, d, parts, teams, group, rows;
     int64_t groups;          // gate rows
+    int by_wave;             // a wave takes a gate row (few teams share one), else the workgroup
     int grouped;
     const float* part;       // [4][parts][d]
     const float* gate_part;  // [teams][2][d]
@@ -522,26 +523,36 @@ struct ResidualFinish {
 // forms the gradient of a single gate row, from two of them); from 4 on: gate
 // rows whose tokens several teams share. Those are found from the ends of the
 // teams' tokens, or, where there are fewer, from the gate rows: a row belongs to
-// the first team's end that lies inside it.
+// the first team's end that lies inside it. A gate row that few teams share is
+// one wave's, so that a workgroup takes as many as it has waves.
 constexpr int kFinishWaves = 16;
 
 __global__ __launch_bounds__(kFinishWaves* kWave) void residual_finish_kernel(ResidualFinish p) {
     __shared__ double stretch[2][kFinishWaves][kWave];
     const int lane = lane_id(), w = (int)threadIdx.x >> 6, n = (int)blockIdx.x * kWave + lane;
-    // sum of count rows of src, `stride` floats apart
-    auto column = [&](const float* src, int64_t count, size_t stride) {
-        const int64_t k0 = w * count / kFinishWaves, k1 = (w + 1) * count / kFinishWaves;
+    // sum of rows k0 to k1 of src, `stride` floats apart
+    auto column = [&](const float* src, int64_t k0, int64_t k1, size_t stride) {
         double s = 0.0;
         int64_t k = k0;
-        for (; k + 8 <= k1; k += 8) {
-            float v[8];
+        for (; k + 16 <= k1; k += 16) {
+            float v[16];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = src[(size_t)(k + u) * stride];
+            for (int u = 0; u < 16; ++u) v[u] = src[(size_t)(k + u) * stride];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) s += (double)v[u];
+            for (int u = 0; u < 16; ++u) s += (double)v[u];
+        }
+        for (; k + 4 <= k1; k += 4) {
+            float v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v[u] = src[(size_t)(k + u) * stride];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) s += (double)v[u];
         }
         for (; k < k1; ++k) s += (double)src[(size_t)k * stride];
         return s;
+    };
+    auto part_of = [&](const float* src, int64_t count, size_t stride) {
+        return column(src, w * count / kFinishWaves, (w + 1) * count / kFinishWaves, stride);
     };
     auto total = [&](int i) {
         double s = 0.0;
@@ -554,8 +565,8 @@ __global__ __launch_bounds__(kFinishWaves* kWave) void residual_finish_kernel(Re
         float* const out = p.d_sum[i];
         if (out == nullptr && !gate) return;
         const float* const src = p.part + (size_t)i * p.parts * p.d + n;
-        stretch[0][w][lane] = n < p.d ? column(src, p.parts, p.d) : 0.0;
-        stretch[1][w][lane] = gate && n < p.d ? column(src + (size_t)p.parts * p.d, p.parts, p.d) : 0.0;
+        stretch[0][w][lane] = n < p.d ? part_of(src, p.parts, p.d) : 0.0;
+        stretch[1][w][lane] = gate && n < p.d ? part_of(src + (size_t)p.parts * p.d, p.parts, p.d) : 0.0;
         __syncthreads();
         if (w != 0 || n >= p.d) return;
         const double s = total(0);
@@ -566,21 +577,30 @@ __global__ __launch_bounds__(kFinishWaves* kWave) void residual_finish_kernel(Re
         return;
     }
     int64_t g = (int64_t)blockIdx.y - 4;
+    if (p.by_wave) g = g * kFinishWaves + w;
+    int64_t first = -1, last = -1;
     if (p.teams - 1 < p.groups) {
-        const int64_t end = (g + 1) * p.rows;   // of team blockIdx.y - 4
+        const int64_t end = (g + 1) * p.rows;   // of team number g
         g = end / p.group;
-        if (end >= p.N || g * p.group == end || end - p.rows > g * p.group) return;
+        if (end < p.N && g * p.group < end && end - p.rows <= g * p.group) first = end / p.rows - 1;
+    } else if (g < p.groups) {
+        first = g * p.group / p.rows;
     }
     const int64_t g0 = g * p.group, g1 = g0 + p.group < p.N ? g0 + p.group : p.N;
-    const int64_t first = g0 / p.rows, last = (g1 - 1) / p.rows;
-    if (first == last) return;
+    if (first >= 0) last = (g1 - 1) / p.rows;
+    const bool shared = first >= 0 && first < last && n < p.d;
+    const float* const rest = p.gate_part + (size_t)(first + 1) * 2 * p.d + n;
     double s = 0.0;
-    if (n < p.d) s = column(p.gate_part + (size_t)(first + 1) * 2 * p.d + n, last - first, (size_t)2 * p.d);
-    stretch[0][w][lane] = s;
-    __syncthreads();
-    if (w == 0 && n < p.d)
+    if (p.by_wave) {
+        if (shared) s = column(rest, 0, last - first, (size_t)2 * p.d);
+    } else {
+        stretch[0][w][lane] = shared ? part_of(rest, last - first, (size_t)2 * p.d) : 0.0;
+        __syncthreads();
+        s = total(0);
+    }
+    if (shared && (p.by_wave || w == 0))
         p.d_gate[(size_t)g * p.d + n] =
-            (float)((double)p.gate_part[((size_t)first * 2 + (g0 > first * p.rows ? 1 : 0)) * p.d + n] + total(0));
+            (float)((double)p.gate_part[((size_t)first * 2 + (g0 > first * p.rows ? 1 : 0)) * p.d + n] + s);
 }
 
 #undef UNIF_COLS
