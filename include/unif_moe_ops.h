@@ -122,6 +122,9 @@ int32_t unif_moe_residual_backward(const unif_moe_residual* res, const void* y, 
                                    void* dx, void* df, const unif_moe_residual_grads* grads, void* workspace,
                                    size_t workspace_bytes, void* stream);
 
+/* Narrowest layers whose balance gradients are formed. */
+#define UNIF_BALANCE_MIN_D 8
+
 /* What an expert's load counts. */
 #define UNIF_BALANCE_TOKENS 0 /* tokens that run the expert                          */
 #define UNIF_BALANCE_BLOCKS 1 /* blocks those tokens run of it: B - b each           */
@@ -166,8 +169,8 @@ int32_t unif_moe_balance_loss_workspace_size(const unif_moe_config* cfg, const u
  * Precision: p, the loads' shares and the gradients in fp32, sums over tokens
  * in fp32 within a workgroup's tokens and in fp64 past that, in a fixed order:
  * repeated calls give the same bits.
- * Errors: UNIF_EINVAL, UNIF_EWORKSPACE, UNIF_EUNSUPPORTED before any launch;
- * UNIF_EDEVICE if a launch fails. */
+ * Errors: UNIF_EINVAL, UNIF_EWORKSPACE, UNIF_EUNSUPPORTED (also gradients of d <
+ * UNIF_BALANCE_MIN_D) before any launch; UNIF_EDEVICE if a launch fails. */
 int32_t unif_moe_balance_loss(const unif_moe_config* cfg, const unif_moe_balance* bal,
                               const unif_moe_routing* record, const uint8_t* valid, const void* X,
                               const float* W_router, float* loss, int64_t* counts, const float* dX_in,

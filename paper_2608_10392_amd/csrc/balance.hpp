@@ -2,10 +2,11 @@
 // and the gradient (include/unif_moe_ops.h).
 //
 // The loads c_sj and the affinities' sums of a group are a pass over the record
-// (8 K bytes a token); the gradient is a second one, whose dl_tj = p_tj (a_sj -
-// sum_m p_tm a_sm), a_sj = weight K c_sj / (G n_s sum_m c_sm), feeds two
-// products, dX += dl W and dW += dl^T X. Reading X and reading and writing dX
-// bound it.
+// (8 K bytes a token). The gradient is a second one: dl_tj = p_tj (a_sj -
+// sum_m p_tm a_sm), a_sj = weight K c_sj / (G n_s sum_m c_sm), feeds the two
+// products dX += dl W and dW += dl^T X. Reading X and reading and writing dX
+// bound it: (2 or 4) + 8 bytes an element against 4 K operations, on the fp32
+// matrix cores.
 #pragma once
 #include "common.hpp"
 
@@ -15,8 +16,8 @@ struct BalanceParams {
     int N, d, K, B;
     int group;             // tokens per group
     int groups;
-    int pieces;            // per group, of `piece` tokens
-    int piece;
+    int pieces;            // workgroups per group in the count
+    int piece;             // tokens of a group per workgroup
     int blocks;            // loads count blocks
     float weight;
     const uint8_t* valid;
@@ -32,94 +33,25 @@ struct BalanceParams {
     float* dW;
     float* loss;
     int64_t* counts;       // [groups, K+1]
-    float* mass;           // [groups, pieces, K] sums of affinities
-    int* load;             // [groups, pieces, K+2]: loads, the shared expert's, valid tokens
+    double* mass;          // [groups, pieces, K] sums of affinities
+    int64_t* load;         // [groups, pieces, K+2]: loads, the shared expert's, valid tokens
     float* slope;          // [groups, K]: a_sj
     double* gloss;         // [groups]: L_s
-    float* dl;             // [N, K]
-    float* part;           // [slices][K][d]
-    int slices;
+    float* part;           // [parts][K][d]: partial dl^T X
+    int parts;             // workgroups along the tokens
+    int steps;             // of 16 tokens, per workgroup
 };
 
-// Loads and affinity sums of one piece of a group per wave: 64 tokens at a
-// time, their affinities put in expert order in LDS (selected experts with the
-// sign bit set), then one lane per expert adds its column.
-constexpr int kBalWaves = 4;
-__host__ __device__ __forceinline__ int balance_lds_words(int K) { return 64 * (K | 1) + 64; }
-
-__global__ __launch_bounds__(64 * kBalWaves) void balance_count_kernel(BalanceParams p) {
-    extern __shared__ float lds[];
-    const int w = (int)threadIdx.x >> 6, lane = lane_id(), K = p.K, ld = K | 1;
-    float* const tile = lds + w * balance_lds_words(K);
-    int* const unit = reinterpret_cast<int*>(tile + 64 * ld);
-    const int64_t u = (int64_t)blockIdx.x * kBalWaves + w;
-    if (u >= (int64_t)p.groups * p.pieces) return;
-    const int64_t g = u / p.pieces, g0 = g * p.group, g1 = g0 + p.group < p.N ? g0 + p.group : p.N;
-    const int64_t t0 = g0 + (u - g * p.pieces) * p.piece, t1 = t0 + p.piece < g1 ? t0 + p.piece : g1;
-    float mass = 0.f;
-    int load = 0, shared = 0, tokens = 0;
-    for (int64_t tb = t0; tb < t1; tb += 64) {
-        const int64_t t = tb + lane;
-        const bool ok = t < t1 && (p.valid == nullptr || p.valid[t] != 0);
-        for (int j = 0; j < K; ++j) tile[lane * ld + j] = 0.f;
-        unit[lane] = 0;
-        if (ok) {
-            const int b = p.blocks ? p.nsh[t] : 0, k = min(p.nres[t], K);
-            unit[lane] = p.blocks ? p.B - b : 1;
-            shared += p.blocks ? b : 1;
-            ++tokens;
-            for (int i = 0; i < K; ++i) {
-                const int e = p.eids[(size_t)t * K + i];
-                if (e < 1 || e > K) continue;
-                const uint32_t v = __float_as_uint(p.wts[(size_t)t * K + i]) & 0x7fffffffu;
-                tile[lane * ld + e - 1] = __uint_as_float(i < k ? v | 0x80000000u : v);
-            }
-        }
-        wait_lgkmcnt0();
-        __builtin_amdgcn_wave_barrier();
-        if (lane < K)
-            for (int q = 0; q < 64; ++q) {
-                const uint32_t v = __float_as_uint(tile[q * ld + lane]);
-                mass += __uint_as_float(v & 0x7fffffffu);
-                if (v >> 31) load += unit[q];
-            }
-        wait_lgkmcnt0();
-        __builtin_amdgcn_wave_barrier();
-    }
-    for (int o = 32; o > 0; o >>= 1) {
-        shared += __shfl_xor(shared, o);
-        tokens += __shfl_xor(tokens, o);
-    }
-    if (lane < K) {
-        p.mass[u * K + lane] = mass;
-        p.load[u * (K + 2) + lane] = load;
-    }
-    if (lane == 0) {
-        p.load[u * (K + 2) + K] = shared;
-        p.load[u * (K + 2) + K + 1] = tokens;
-    }
-}
-
 __device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
     return v;
 }
 
-// One wave per group: the pieces' sums in order, the counts, L_s and the slopes.
-__global__ __launch_bounds__(64) void balance_group_kernel(BalanceParams p) {
-    const int64_t g = blockIdx.x;
+// A group's sums, lane j those of expert j: its counts, L_s and slopes.
+__device__ __forceinline__ void balance_finish_group(const BalanceParams& p, int64_t g, double mass, int64_t load,
+                                                     int64_t shared, int64_t tokens) {
     const int lane = lane_id(), K = p.K;
-    double mass = 0.0;
-    int64_t load = 0, shared = 0, tokens = 0;
-    for (int q = 0; q < p.pieces; ++q) {
-        const int64_t u = g * p.pieces + q;
-        if (lane < K) {
-            mass += (double)p.mass[u * K + lane];
-            load += p.load[u * (K + 2) + lane];
-        }
-        shared += p.load[u * (K + 2) + K];
-        tokens += p.load[u * (K + 2) + K + 1];
-    }
     const double total = wave_sum((double)load), n = (double)tokens;
     const bool some = tokens > 0 && total > 0.0;
     const double share = some ? (double)load / total : 0.0;
@@ -129,94 +61,411 @@ __global__ __launch_bounds__(64) void balance_group_kernel(BalanceParams p) {
         if (lane == 0) p.counts[g * (K + 1)] = shared;
     }
     if (lane < K) p.slope[g * K + lane] = some ? (float)((double)p.weight * K * share / (n * (double)p.groups)) : 0.f;
-    if (lane == 0) p.gloss[g] = l;
+    if (lane == 0) {
+        p.gloss[g] = l;
+        if (p.groups == 1) *p.loss = (float)l;
+    }
 }
 
-// *loss = the groups' mean, 256 strided partial sums and a fixed tree.
-__global__ __launch_bounds__(256) void balance_loss_kernel(BalanceParams p) {
-    __shared__ double part[256];
+// Loads and affinity sums of one piece of a group per workgroup. A wave takes
+// 64 tokens at a time: the record's entries are read side by side and put in
+// expert order in LDS (selected experts with the sign bit set), then lane j +
+// w h adds expert j's entries of the h-th of 64 / w runs of tokens, w the
+// experts rounded up to a power of two. A group of one piece is finished here.
+constexpr int kBalWaves = 4;
+__host__ __device__ __forceinline__ int balance_wave_words(int K) { return 64 * (K | 1) + 2 * 64; }
+
+__global__ __launch_bounds__(kWave* kBalWaves) void balance_count_kernel(BalanceParams p) {
+    extern __shared__ float lds[];
+    __shared__ double masses[kBalWaves][kWave];
+    __shared__ int loads[kBalWaves][kWave + 2];
+    const int w = (int)threadIdx.x >> 6, nw = (int)blockDim.x >> 6, lane = lane_id(), K = p.K, ld = K | 1;
+    float* const tile = lds + w * balance_wave_words(K);
+    int* const unit = reinterpret_cast<int*>(tile + 64 * ld);   // what a selected expert of the token counts
+    int* const chosen = unit + 64;                              // experts selected, -1: padded
+    const int64_t u = (int64_t)flat_block();
+    if (u >= (int64_t)p.groups * p.pieces) return;
+    const int64_t g = u / p.pieces, g0 = g * p.group, g1 = g0 + p.group < p.N ? g0 + p.group : p.N;
+    const int64_t t0 = g0 + (u - g * p.pieces) * p.piece, t1 = t0 + p.piece < g1 ? t0 + p.piece : g1;
+    const int wide = K <= 1 ? 1 : 1 << (32 - __builtin_clz(K - 1));
+    const int j = lane & (wide - 1), h = lane / wide, run = wide;   // 64 / (64 / wide) tokens per run
+    double mass = 0.0;
+    int load = 0, shared = 0, tokens = 0;
+    for (int64_t tb = t0 + 64 * w; tb < t1; tb += 64 * nw) {
+        const int64_t t = tb + lane;
+        const bool ok = t < t1 && (p.valid == nullptr || p.valid[t] != 0);
+        const int b = ok && p.blocks ? p.nsh[t] : 0;
+        unit[lane] = p.blocks ? p.B - b : 1;
+        chosen[lane] = ok ? min(p.nres[t], K) : -1;
+        if (ok) {
+            shared += p.blocks ? b : 1;
+            ++tokens;
+        }
+        for (int i = lane; i < 64 * ld; i += kWave) tile[i] = 0.f;
+        wait_lgkmcnt0();
+        __builtin_amdgcn_wave_barrier();
+        const int entries = (int)(t1 - tb < 64 ? t1 - tb : 64) * K;
+        const int* const ids = p.eids + (size_t)tb * K;
+        const float* const wts = p.wts + (size_t)tb * K;
+        int q = lane / K, r = lane - q * K;         // token and rank of entry `lane`
+        const int dq = kWave / K, dr = kWave - dq * K;
+        for (int i0 = lane; i0 < entries; i0 += 8 * kWave) {
+            int e[8];
+            float v[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                const int i = i0 + c * kWave;
+                e[c] = i < entries ? ids[i] : 0;
+                v[c] = i < entries ? wts[i] : 0.f;
+            }
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                if (e[c] >= 1 && e[c] <= K && chosen[q] >= 0)
+                    tile[q * ld + e[c] - 1] =
+                        __uint_as_float((__float_as_uint(v[c]) & 0x7fffffffu) | (r < chosen[q] ? 0x80000000u : 0u));
+                q += dq;
+                r += dr;
+                if (r >= K) {
+                    r -= K;
+                    ++q;
+                }
+                q = min(q, 63);   // past the last entry
+            }
+        }
+        wait_lgkmcnt0();
+        __builtin_amdgcn_wave_barrier();
+        if (j < K) {
+            float m = 0.f;
+            for (int i = 0; i < run; ++i) {
+                const uint32_t v = __float_as_uint(tile[(h * run + i) * ld + j]);
+                m += __uint_as_float(v & 0x7fffffffu);
+                load += (v >> 31) ? unit[h * run + i] : 0;
+            }
+            mass += (double)m;
+        }
+        wait_lgkmcnt0();
+        __builtin_amdgcn_wave_barrier();
+    }
+    for (int o = 32; o >= wide; o >>= 1) {
+        mass += __shfl_xor(mass, o);
+        load += __shfl_xor(load, o);
+    }
+    for (int o = 32; o > 0; o >>= 1) {
+        shared += __shfl_xor(shared, o);
+        tokens += __shfl_xor(tokens, o);
+    }
+    masses[w][lane] = mass;
+    loads[w][lane] = load;
+    if (lane == 0) {
+        loads[w][kWave] = shared;
+        loads[w][kWave + 1] = tokens;
+    }
+    __syncthreads();
+    if (w != 0) return;
+    double m = 0.0;
+    int64_t l = 0, s = 0, n = 0;
+    for (int i = 0; i < nw; ++i) {
+        if (lane < K) {
+            m += masses[i][lane];
+            l += loads[i][lane];
+        }
+        s += loads[i][kWave];
+        n += loads[i][kWave + 1];
+    }
+    if (p.pieces == 1) {
+        balance_finish_group(p, g, m, l, s, n);
+        return;
+    }
+    if (lane < K) {
+        p.mass[u * K + lane] = m;
+        p.load[u * (K + 2) + lane] = l;
+    }
+    if (lane == 0) {
+        p.load[u * (K + 2) + K] = s;
+        p.load[u * (K + 2) + K + 1] = n;
+    }
+}
+
+// One workgroup per group of several pieces: each wave adds a stretch of them.
+constexpr int kBalGroupWaves = 16;
+__global__ __launch_bounds__(kWave* kBalGroupWaves) void balance_group_kernel(BalanceParams p) {
+    __shared__ double masses[kBalGroupWaves][kWave];
+    __shared__ int64_t loads[kBalGroupWaves][kWave + 2];
+    const int64_t g = (int64_t)flat_block();
+    if (g >= p.groups) return;
+    const int lane = lane_id(), w = (int)threadIdx.x >> 6, K = p.K;
+    const int q0 = (int)((int64_t)w * p.pieces / kBalGroupWaves), q1 = (int)((int64_t)(w + 1) * p.pieces / kBalGroupWaves);
+    double mass = 0.0;
+    int64_t load = 0, shared = 0, tokens = 0;
+    for (int q = q0; q < q1; q += 8) {
+        double m[8];
+        int64_t l[8], s[8], n[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            const int64_t u = g * p.pieces + min(q + c, q1 - 1);
+            m[c] = p.mass[u * K + min(lane, K - 1)];
+            l[c] = p.load[u * (K + 2) + min(lane, K - 1)];
+            s[c] = p.load[u * (K + 2) + K];
+            n[c] = p.load[u * (K + 2) + K + 1];
+        }
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            if (q + c >= q1) continue;
+            mass += m[c];
+            load += l[c];
+            shared += s[c];
+            tokens += n[c];
+        }
+    }
+    masses[w][lane] = mass;
+    loads[w][lane] = load;
+    if (lane == 0) {
+        loads[w][kWave] = shared;
+        loads[w][kWave + 1] = tokens;
+    }
+    __syncthreads();
+    if (w != 0) return;
+    mass = 0.0;
+    load = shared = tokens = 0;
+    for (int i = 0; i < kBalGroupWaves; ++i) {
+        if (lane < K) {
+            mass += masses[i][lane];
+            load += loads[i][lane];
+        }
+        shared += loads[i][kWave];
+        tokens += loads[i][kWave + 1];
+    }
+    balance_finish_group(p, g, mass, load, shared, tokens);
+}
+
+// *loss = the groups' mean: strided partial sums, a wave's by a butterfly, the
+// waves in order.
+__device__ __forceinline__ void balance_mean(const BalanceParams& p) {
+    __shared__ double part[16];
+    const int nw = (int)blockDim.x >> 6, w = (int)threadIdx.x >> 6;
     double s = 0.0;
-    for (int64_t g = threadIdx.x; g < p.groups; g += 256) s += p.gloss[g];
-    part[threadIdx.x] = s;
+    for (int64_t g = threadIdx.x; g < p.groups; g += blockDim.x) s += p.gloss[g];
+    s = wave_sum(s);
+    if (lane_id() == 0) part[w] = s;
     __syncthreads();
-    for (int h = 128; h > 0; h >>= 1) {
-        if ((int)threadIdx.x < h) part[threadIdx.x] += part[threadIdx.x + h];
+    if (threadIdx.x != 0) return;
+    s = 0.0;
+    for (int i = 0; i < nw; ++i) s += part[i];
+    *p.loss = p.groups > 0 ? (float)(s / p.groups) : 0.f;
+}
+__global__ __launch_bounds__(1024) void balance_mean_kernel(BalanceParams p) { balance_mean(p); }
+
+// The gradients of 16 steps tokens per workgroup. Its waves hold 16 NC columns
+// each, lane l the NC consecutive ones from 16-lane column l % 16 on, so that one
+// load gives a lane its operand of NC products (product i stands for every NC-th
+// column): for v_mfma_f32_16x16x4_f32, X[t + l / 16] is the right operand of
+// dl^T X and W_j the one of dl W, whose sums dX_in is added to. The router's rows
+// and the sums of dl^T X stay in registers. The next 16 tokens' rows are loaded
+// while the current ones are multiplied. dl of 64 tokens at a time is formed by
+// all waves in LDS (zeros for padded tokens, whose rows of X are not used).
+// NC = 8 up to 32 experts, 4 past that: the registers then hold two waves per
+// SIMD.
+constexpr int kBalTile = 64;
+
+template <class T, int NC>
+struct BalRow {
+    typedef T mem __attribute__((ext_vector_type(NC), aligned(sizeof(T))));
+};
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(u16 v) { return bf2f(v); }
+
+template <class T, int KT, int NC>
+__global__ __launch_bounds__(512, 2) void balance_grad_kernel(BalanceParams p) {
+    constexpr int KP = 16 * KT, LD = KP + 4;   // LDS row: the 16 rows' reads of 4 neighbours meet no bank twice
+    __shared__ float dls[kBalTile * LD];
+    __shared__ float means[8][kBalTile];
+    if ((int)blockIdx.x == p.parts) {   // one workgroup more than the tokens need: the groups' mean
+        if (blockIdx.y == 0) balance_mean(p);
+        return;
+    }
+    typedef typename BalRow<T, NC>::mem x_mem;
+    typedef typename BalRow<float, NC>::mem f_mem;
+    typedef T x_raw __attribute__((ext_vector_type(NC)));
+    typedef float f_raw __attribute__((ext_vector_type(NC)));
+    const int lane = lane_id(), w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), nw = (int)blockDim.x >> 6;
+    const int lr = lane & 15, lq = lane >> 4, K = p.K;
+    // This lane's columns: from col on, loaded from at (the row's last NC where
+    // fewer are left); columns before col belong to other lanes.
+    const int col = (((int)blockIdx.y * nw + w) * 16 + lr) * NC;
+    const uint32_t at = (uint32_t)min(col, p.d - NC);
+    const int own = (int)at >= col ? 0 : min(col - (int)at, NC);   // first own element (NC: none)
+    const int64_t first = (int64_t)blockIdx.x * p.steps * 16;
+    const int64_t end = first + p.steps * 16 < p.N ? first + p.steps * 16 : p.N;
+    const bool add = p.dX_in != nullptr;
+
+    f_raw W[4 * KT];
+#pragma unroll
+    for (int kk = 0; kk < 4 * KT; ++kk) {
+        const int j = 4 * kk + lq;
+        W[kk] = f_raw{};
+        if (p.dX != nullptr && j < K) W[kk] = *reinterpret_cast<const f_mem*>(p.Wr + (size_t)(j + 1) * p.d + at);
+    }
+    f32x4 dW[KT][NC];
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int i = 0; i < NC; ++i) dW[kt][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    x_raw x[4];   // rows t + 4 q + lq of X
+    f_raw s[4];   // rows t + 4 lq + r of dX_in
+    // A step's rows have a scalar base and a lane's 32-bit offset; rows past the
+    // last token are read as the last one and used nowhere.
+    const uint32_t xoff = ((uint32_t)lq * p.d + at) * (uint32_t)sizeof(T), soff = ((uint32_t)lq * 4 * p.d + at) * 4u;
+    auto load_x = [&](int64_t t) {
+        if (p.dW == nullptr) return;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int64_t row = t + 4 * q < p.N ? t + 4 * q : p.N - 1;
+            uint32_t off = xoff;
+            if (t + 16 > p.N) off = ((uint32_t)min((int64_t)lq, p.N - 1 - row) * p.d + at) * (uint32_t)sizeof(T);
+            x[q] = *reinterpret_cast<const x_mem*>(static_cast<const char*>(p.X) + (size_t)row * p.d * sizeof(T) + off);
+        }
+    };
+    auto load_s = [&](int64_t t) {
+        if (!add) return;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int64_t row = t + r < p.N ? t + r : p.N - 1;
+            uint32_t off = soff;
+            if (t + 16 > p.N) off = ((uint32_t)min((int64_t)lq * 4, p.N - 1 - row) * p.d + at) * 4u;
+            s[r] = *reinterpret_cast<const f_mem*>(reinterpret_cast<const char*>(p.dX_in) + (size_t)row * p.d * 4 + off);
+        }
+    };
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s[r] = f_raw{};
+    load_x(first);
+    load_s(first);
+    for (int64_t tb = first; tb < end; tb += kBalTile) {
+        // dl of this tile's tokens (lane: token), the entries dealt to the waves
+        const int64_t t = tb + lane;
+        const bool ok = t < end && (p.valid == nullptr || p.valid[t] != 0);
+        const uint64_t real = ballot(ok);
+        __syncthreads();   // the last tile's dl is used up
+        for (int i = threadIdx.x; i < kBalTile * LD; i += blockDim.x) dls[i] = 0.f;
+        const float* const slope = p.slope + (ok ? t / p.group : 0) * K;
+        const int* const ids = p.eids + (size_t)(ok ? t : first) * K;
+        const float* const wts = p.wts + (size_t)(ok ? t : first) * K;
+        float m = 0.f;
+        for (int i = w; i < K; i += nw) {
+            const int e = ids[i];
+            const float v = wts[i];
+            if (ok && e >= 1 && e <= K) m = fmaf(v, slope[e - 1], m);
+        }
+        means[w][lane] = m;
         __syncthreads();
+        m = 0.f;
+        for (int i = 0; i < nw; ++i) m += means[i][lane];
+        for (int i = w; i < K; i += nw) {
+            const int e = ids[i];
+            const float v = wts[i];
+            if (ok && e >= 1 && e <= K) dls[lane * LD + e - 1] = v * (slope[e - 1] - m);
+        }
+        __syncthreads();
+        for (int64_t t16 = tb; t16 < end && t16 < tb + kBalTile; t16 += 16) {
+            const int in_tile = (int)(t16 - tb);
+            const uint32_t mask = (uint32_t)(real >> in_tile) & 0xffffu;
+            const bool more = t16 + 16 < end;
+            const float* const dl = dls + in_tile * LD;
+            if (p.dW != nullptr) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float b[NC];
+#pragma unroll
+                    for (int i = 0; i < NC; ++i) b[i] = to_f32(x[q][i]);
+                    if (mask != 0xffffu) {
+                        const bool on = mask >> (4 * q + lq) & 1;
+#pragma unroll
+                        for (int i = 0; i < NC; ++i) b[i] = on ? b[i] : 0.f;
+                    }
+#pragma unroll
+                    for (int kt = 0; kt < KT; ++kt) {
+                        const float a = dl[(4 * q + lq) * LD + 16 * kt + lr];
+#pragma unroll
+                        for (int i = 0; i < NC; ++i)
+                            dW[kt][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, b[i], dW[kt][i], 0, 0, 0);
+                    }
+                }
+                if (more) load_x(t16 + 16);
+            }
+            if (p.dX != nullptr) {
+                f32x4 acc[NC];
+#pragma unroll
+                for (int i = 0; i < NC; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int kk = 0; kk < 4 * KT; ++kk) {
+                    const float a = dl[lr * LD + 4 * kk + lq];
+#pragma unroll
+                    for (int i = 0; i < NC; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, W[kk][i], acc[i], 0, 0, 0);
+                }
+                f_raw v[4];   // dX_in is added last: one rounding at its magnitude
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int i = 0; i < NC; ++i) v[r][i] = s[r][i] + acc[i][r];
+                if (more) load_s(t16 + 16);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    if (t16 + 4 * lq + r >= end) continue;
+                    char* const out = reinterpret_cast<char*>(p.dX) + (size_t)(t16 + r) * p.d * 4 + soff;
+                    if (own == 0) *reinterpret_cast<f_mem*>(out) = v[r];
+                    else
+#pragma unroll
+                        for (int i = 0; i < NC; ++i)
+                            if (i >= own) reinterpret_cast<float*>(out)[i] = v[r][i];
+                }
+            }
+        }
     }
-    if (threadIdx.x == 0) *p.loss = p.groups > 0 ? (float)(part[0] / p.groups) : 0.f;
-}
-
-// dl of every token, one thread each.
-__global__ __launch_bounds__(256) void balance_dl_kernel(BalanceParams p) {
-    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (t >= p.N) return;
-    const int K = p.K;
-    float* const dl = p.dl + (size_t)t * K;
-    for (int j = 0; j < K; ++j) dl[j] = 0.f;
-    if (p.valid != nullptr && p.valid[t] == 0) return;
-    const float* const slope = p.slope + t / p.group * K;
-    float mean = 0.f;
-    for (int i = 0; i < K; ++i) {
-        const int e = p.eids[(size_t)t * K + i];
-        if (e >= 1 && e <= K) mean = fmaf(p.wts[(size_t)t * K + i], slope[e - 1], mean);
-    }
-    for (int i = 0; i < K; ++i) {
-        const int e = p.eids[(size_t)t * K + i];
-        if (e >= 1 && e <= K) dl[e - 1] = p.wts[(size_t)t * K + i] * (slope[e - 1] - mean);
-    }
-}
-
-template <class T>
-__device__ __forceinline__ float to_f32(T v) { return v; }
-template <>
-__device__ __forceinline__ float to_f32<u16>(u16 v) { return bf2f(v); }
-
-// dX = dX_in + dl W, 16 tokens x 256 columns per workgroup.
-__global__ __launch_bounds__(256) void balance_dx_kernel(BalanceParams p) {
-    __shared__ float dls[16][64];
-    const int64_t t0 = (int64_t)blockIdx.x * 16;
-    const int n = (int)blockIdx.y * 256 + (int)threadIdx.x, K = p.K;
-    for (int x = threadIdx.x; x < 16 * K; x += 256) dls[x / K][x % K] = t0 + x / K < p.N ? p.dl[(size_t)t0 * K + x] : 0.f;
-    __syncthreads();
-    if (n >= p.d) return;
-    float acc[16];
-    for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-    for (int j = 0; j < K; ++j) {
-        const float w = p.Wr[(size_t)(j + 1) * p.d + n];
-        for (int i = 0; i < 16; ++i) acc[i] = fmaf(dls[i][j], w, acc[i]);
-    }
-    for (int i = 0; i < 16; ++i)
-        if (t0 + i < p.N) {
-            const size_t at = (size_t)(t0 + i) * p.d + n;
-            p.dX[at] = p.dX_in != nullptr ? p.dX_in[at] + acc[i] : acc[i];
+    if (p.dW == nullptr) return;
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int j = 16 * kt + 4 * lq + r;
+            if (j >= K) continue;
+            float* const out = p.part + ((size_t)blockIdx.x * K + j) * p.d + at;
+            f_raw v;
+#pragma unroll
+            for (int i = 0; i < NC; ++i) v[i] = dW[kt][i][r];
+            if (own == 0) *reinterpret_cast<f_mem*>(out) = v;
+            else
+#pragma unroll
+                for (int i = 0; i < NC; ++i)
+                    if (i >= own) out[i] = v[i];
         }
 }
 
-// Partial dl^T X of one slice of the tokens: a thread per column, 8 experts at
-// a time. Padded tokens' rows are not read.
-template <class T>
-__global__ __launch_bounds__(256) void balance_dw_kernel(BalanceParams p) {
-    const int n = (int)blockIdx.x * 256 + (int)threadIdx.x, K = p.K, j0 = (int)blockIdx.y * 8;
-    const int64_t t0 = (int64_t)blockIdx.z * p.N / p.slices, t1 = (int64_t)(blockIdx.z + 1) * p.N / p.slices;
-    if (n >= p.d) return;
-    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int64_t t = t0; t < t1; ++t) {
-        if (p.valid != nullptr && p.valid[t] == 0) continue;
-        const float x = to_f32(static_cast<const T*>(p.X)[(size_t)t * p.d + n]);
-        for (int j = 0; j < 8; ++j)
-            if (j0 + j < K) acc[j] = fmaf(p.dl[(size_t)t * K + j0 + j], x, acc[j]);
+// dW = dW_in + the parts' sum (row 0: dW_in): 64 elements per workgroup, each
+// wave a stretch of the parts, all in fp64 and in order.
+constexpr int kBalSumWaves = 16;
+__global__ __launch_bounds__(kWave* kBalSumWaves) void balance_dw_sum_kernel(BalanceParams p) {
+    __shared__ double stretch[kBalSumWaves][kWave];
+    const int lane = lane_id(), w = (int)threadIdx.x >> 6;
+    const size_t n = (size_t)p.K * p.d, i = (size_t)blockIdx.x * kWave + lane;   // over all K + 1 rows
+    const size_t k0 = (size_t)w * p.parts / kBalSumWaves, k1 = (size_t)(w + 1) * p.parts / kBalSumWaves;
+    double s = 0.0;
+    if (i >= (size_t)p.d && i < n + p.d) {
+        const float* const src = p.part + (i - p.d);
+        size_t k = k0;
+        for (; k + 8 <= k1; k += 8) {
+            float v[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) v[c] = src[(k + c) * n];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) s += (double)v[c];
+        }
+        for (; k < k1; ++k) s += (double)src[k * n];
     }
-    for (int j = 0; j < 8; ++j)
-        if (j0 + j < K) p.part[((size_t)blockIdx.z * K + j0 + j) * p.d + n] = acc[j];
-}
-
-// dW = dW_in + the slices' sum in order (row 0: dW_in).
-__global__ __launch_bounds__(256) void balance_dw_sum_kernel(BalanceParams p) {
-    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, n = (size_t)(p.K + 1) * p.d;
-    if (i >= n) return;
-    double s = p.dW_in != nullptr ? (double)p.dW_in[i] : 0.0;
-    if (i >= (size_t)p.d)
-        for (int k = 0; k < p.slices; ++k) s += (double)p.part[(size_t)k * (n - p.d) + i - p.d];
+    stretch[w][lane] = s;
+    __syncthreads();
+    if (w != 0 || i >= n + p.d) return;
+    s = p.dW_in != nullptr ? (double)p.dW_in[i] : 0.0;
+    for (int k = 0; k < kBalSumWaves; ++k) s += stretch[k][lane];
     p.dW[i] = (float)s;
 }
 

@@ -49,6 +49,13 @@ struct Carver {
 
 inline size_t ceil_div_sz(size_t a, size_t b) { return (a + b - 1) / b; }
 
+// A grid of at least `blocks` workgroups, numbered by flat_block(): the threads
+// of a grid's x dimension are limited to 2^32 - 1.
+inline dim3 flat_grid(size_t blocks) {
+    const size_t x = (size_t)1 << 22;
+    return blocks <= x ? dim3((unsigned)blocks) : dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
+}
+
 inline char* align_base(void* ws) {
     const uintptr_t a = reinterpret_cast<uintptr_t>(ws);
     return reinterpret_cast<char*>((a + 255) & ~(uintptr_t)255);

@@ -338,40 +338,70 @@ int32_t check_balance(const unif_moe_config* c, const unif_moe_balance* b) {
     const int32_t s = check_config(c);
     if (s != UNIF_OK) return s;
     if (b == nullptr || b->tokens_per_group < 0 || !std::isfinite(b->weight)) return UNIF_EINVAL;
+    if (c->d_model > 1 << 24) return UNIF_EUNSUPPORTED;   // 32-bit offsets inside 16 rows
     if (b->unit != UNIF_BALANCE_TOKENS && b->unit != UNIF_BALANCE_BLOCKS) return UNIF_EINVAL;
     return UNIF_OK;
 }
 
-constexpr int kBalPiece = 256;    // tokens per piece of a group
-constexpr int kBalSlices = 64;
+// Groups of up to this many tokens are one workgroup's in the count, which then
+// finishes them; longer ones are counted in pieces of kBalPiece.
+// Token ranges of the gradient: as many workgroups as run at once, two or more per
+// compute unit, so that the partial sums are few.
+constexpr int kBalParts = 512;
+constexpr int kBalOnePiece = 1024, kBalPiece = 256;
 
 struct BalanceShape {
-    int group, groups, pieces;
+    int group, groups, pieces, piece, waves;   // count
+    int nc, cols, slabs, parts, steps;         // gradient
 };
 BalanceShape balance_shape(const unif_moe_config* c, const unif_moe_balance* b) {
     BalanceShape s;
-    s.group = b->tokens_per_group > 0 ? b->tokens_per_group : std::max(c->n_tokens, 1);
+    const int N = std::max(c->n_tokens, 1);
+    s.group = b->tokens_per_group > 0 ? b->tokens_per_group : N;
     s.groups = b->tokens_per_group > 0 ? ceil_div(c->n_tokens, s.group) : 1;
-    s.pieces = ceil_div(std::min(s.group, std::max(c->n_tokens, 1)), kBalPiece);
+    const int longest = std::min(s.group, N);
+    s.piece = longest <= kBalOnePiece ? longest : kBalPiece;
+    s.pieces = ceil_div(longest, s.piece);
+    s.waves = std::min(kBalWaves, ceil_div(s.piece, 64));
+    // Columns per lane; waves of 16 lanes' columns, at most 8 per workgroup.
+    s.nc = c->n_experts <= 32 ? 8 : 4;
+    const int waves = ceil_div(c->d_model, 16 * s.nc);
+    s.slabs = ceil_div(waves, 8);
+    s.cols = ceil_div(waves, s.slabs);
+    // Token ranges of whole 16-token steps.
+    const int steps = ceil_div(N, 16);
+    s.steps = ceil_div(steps, kBalParts);
+    s.parts = ceil_div(steps, s.steps);
     return s;
 }
 
 struct BalancePlan {
-    size_t mass, load, slope, gloss, dl, part, total;
+    size_t mass, load, slope, gloss, part, total;
 };
 BalancePlan plan_balance(const unif_moe_config* c, const unif_moe_balance* b) {
     const BalanceShape s = balance_shape(c, b);
-    const size_t K = c->n_experts, units = (size_t)s.groups * s.pieces;
+    const size_t K = c->n_experts, units = s.pieces > 1 ? (size_t)s.groups * s.pieces : 0;
     Carver cv;
     BalancePlan p;
-    p.mass = cv.take(4 * units * K);
-    p.load = cv.take(4 * units * (K + 2));
+    p.mass = cv.take(8 * units * K);
+    p.load = cv.take(8 * units * (K + 2));
     p.slope = cv.take(4 * s.groups * K);
     p.gloss = cv.take(8 * (size_t)s.groups);
-    p.dl = cv.take(4 * K * c->n_tokens);
-    p.part = cv.take(4 * (size_t)kBalSlices * K * c->d_model);
+    p.part = cv.take(4 * (size_t)s.parts * K * c->d_model);
     p.total = cv.cur + 256;
     return p;
+}
+
+template <class T>
+void launch_balance_grad(const BalanceShape& s, const BalanceParams& p, unsigned extra, hipStream_t st) {
+    const dim3 grid((unsigned)s.parts + extra, (unsigned)s.slabs);
+    const unsigned threads = (unsigned)s.cols * kWave;
+    switch (ceil_div(p.K, 16)) {
+        case 1: balance_grad_kernel<T, 1, 8><<<grid, threads, 0, st>>>(p); break;
+        case 2: balance_grad_kernel<T, 2, 8><<<grid, threads, 0, st>>>(p); break;
+        case 3: balance_grad_kernel<T, 3, 4><<<grid, threads, 0, st>>>(p); break;
+        default: balance_grad_kernel<T, 4, 4><<<grid, threads, 0, st>>>(p); break;
+    }
 }
 
 }  // namespace
@@ -397,6 +427,7 @@ int32_t unif_moe_balance_loss(const unif_moe_config* cfg, const unif_moe_balance
     if (N > 0 && (!record_complete(record) || (dX != nullptr && W_router == nullptr) ||
                   (dW_router != nullptr && X == nullptr)))
         return UNIF_EINVAL;
+    if ((dX != nullptr || dW_router != nullptr) && d < UNIF_BALANCE_MIN_D) return UNIF_EUNSUPPORTED;
     if ((dX == nullptr && dX_in != nullptr) || (dW_router == nullptr && dW_router_in != nullptr)) return UNIF_EINVAL;
     if (!aligned_to(X, elem_size(cfg->dtype)) || !aligned_to(counts, 8)) return UNIF_EINVAL;
     for (const void* q : {(const void*)W_router, (const void*)loss, (const void*)dX_in, (const void*)dX,
@@ -425,7 +456,7 @@ int32_t unif_moe_balance_loss(const unif_moe_config* cfg, const unif_moe_balance
     p.group = sh.group;
     p.groups = sh.groups;
     p.pieces = sh.pieces;
-    p.piece = kBalPiece;
+    p.piece = sh.piece;
     p.blocks = bal->unit == UNIF_BALANCE_BLOCKS;
     p.weight = bal->weight;
     p.valid = valid;
@@ -441,43 +472,40 @@ int32_t unif_moe_balance_loss(const unif_moe_config* cfg, const unif_moe_balance
     p.dW = dW_router;
     p.loss = loss;
     p.counts = counts;
-    p.mass = reinterpret_cast<float*>(ws + plan.mass);
-    p.load = reinterpret_cast<int*>(ws + plan.load);
+    p.mass = reinterpret_cast<double*>(ws + plan.mass);
+    p.load = reinterpret_cast<int64_t*>(ws + plan.load);
     p.slope = reinterpret_cast<float*>(ws + plan.slope);
     p.gloss = reinterpret_cast<double*>(ws + plan.gloss);
-    p.dl = reinterpret_cast<float*>(ws + plan.dl);
     p.part = reinterpret_cast<float*>(ws + plan.part);
-    p.slices = N > 0 ? kBalSlices : 0;
+    p.parts = N > 0 ? sh.parts : 0;
+    p.steps = sh.steps;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (sh.groups > 0) {
-        const int64_t units = (int64_t)sh.groups * sh.pieces;
-        const size_t lds = sizeof(float) * kBalWaves * (size_t)balance_lds_words(K);
-        if (lds > 64 * 1024 && hipFuncSetAttribute(reinterpret_cast<const void*>(balance_count_kernel),
-                                                   hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
+        const size_t lds = sizeof(float) * sh.waves * (size_t)balance_wave_words(K);
+        if (lds > 64 * 1024 - 4096 && hipFuncSetAttribute(reinterpret_cast<const void*>(balance_count_kernel),
+                                                          hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
             return UNIF_EDEVICE;
-        balance_count_kernel<<<(unsigned)((units + kBalWaves - 1) / kBalWaves), 64 * kBalWaves, lds, st>>>(p);
+        balance_count_kernel<<<flat_grid((size_t)sh.groups * sh.pieces), (unsigned)sh.waves * kWave, lds, st>>>(p);
         UNIF_LAUNCH_CHECK();
-        balance_group_kernel<<<(unsigned)sh.groups, 64, 0, st>>>(p);
+        if (sh.pieces > 1) {
+            balance_group_kernel<<<flat_grid((size_t)sh.groups), kWave * kBalGroupWaves, 0, st>>>(p);
+            UNIF_LAUNCH_CHECK();
+        }
+    }
+    // The groups' mean: with one group it is written already, else beside the
+    // gradients where those are wanted.
+    const bool grads = N > 0 && (dX != nullptr || dW_router != nullptr), mean = sh.groups != 1;
+    if (mean && !grads) {
+        balance_mean_kernel<<<1, 1024, 0, st>>>(p);
         UNIF_LAUNCH_CHECK();
     }
-    balance_loss_kernel<<<1, 256, 0, st>>>(p);
-    UNIF_LAUNCH_CHECK();
-    if (N > 0 && (dX != nullptr || dW_router != nullptr)) {
-        balance_dl_kernel<<<(unsigned)ceil_div(N, 256), 256, 0, st>>>(p);
-        UNIF_LAUNCH_CHECK();
-    }
-    if (N > 0 && dX != nullptr) {
-        balance_dx_kernel<<<dim3((unsigned)ceil_div(N, 16), (unsigned)ceil_div(d, 256)), 256, 0, st>>>(p);
+    if (grads) {
+        if (cfg->dtype == UNIF_BF16) launch_balance_grad<u16>(sh, p, mean, st);
+        else launch_balance_grad<float>(sh, p, mean, st);
         UNIF_LAUNCH_CHECK();
     }
     if (dW_router != nullptr) {
-        if (N > 0) {
-            const dim3 grid((unsigned)ceil_div(d, 256), (unsigned)ceil_div(K, 8), kBalSlices);
-            if (cfg->dtype == UNIF_BF16) balance_dw_kernel<u16><<<grid, 256, 0, st>>>(p);
-            else balance_dw_kernel<float><<<grid, 256, 0, st>>>(p);
-            UNIF_LAUNCH_CHECK();
-        }
-        balance_dw_sum_kernel<<<(unsigned)ceil_div_sz((size_t)(K + 1) * d, 256), 256, 0, st>>>(p);
+        balance_dw_sum_kernel<<<(unsigned)ceil_div_sz((size_t)(K + 1) * d, kWave), kWave * kBalSumWaves, 0, st>>>(p);
         UNIF_LAUNCH_CHECK();
     }
     return UNIF_OK;

@@ -224,13 +224,6 @@ unif_moe_config worst_case(unif_moe_config c) {
 
 // Counters per tile of the permutation: rows per slab, then pairs per expert.
 size_t tile_counters(const Dims& m) { return (size_t)m.nslab + m.K1; }
-// A grid of at least `blocks` workgroups, numbered by flat_block(): the threads
-// of a grid's x dimension are limited to 2^32 - 1.
-dim3 flat_grid(size_t blocks) {
-    const size_t x = (size_t)1 << 22;
-    return blocks <= x ? dim3((unsigned)blocks) : dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
-}
-
 // The post-LN merge takes one wave per token from this many tokens (32 waves
 // per compute unit) of rows of at most kPostWaveChunks chunks, else a workgroup
 // of a thread per chunk, up to four waves, which wait for each other twice.

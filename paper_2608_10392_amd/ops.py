@@ -13,6 +13,7 @@ from ._lib import EINVAL, UnifMoeError, alloc_workspace  # noqa: F401
 ROW_NORMS = {"none": 0, "layer": 1, "rms": 2}
 BALANCE_UNITS = {"tokens": 0, "blocks": 1}
 RESIDUAL_MIN_D, RESIDUAL_MAX_D = 4, 8192
+BALANCE_MIN_D = 8
 PARAMS = ("out_gamma", "out_beta", "in_gamma", "in_beta", "gate")
 
 

@@ -115,7 +115,7 @@ def test_expert_counts(K):
             check(Case(333, d, K, dtype=dtype, unit=unit, per=0 if K % 2 else 50), f"333 x {d} K={K} {dtype} {unit}")
 
 
-@pytest.mark.parametrize("dtype, d", [("f32", 1), ("f32", 3), ("f32", 127), ("f32", 128), ("f32", 130), ("f32", 1025),
+@pytest.mark.parametrize("dtype, d", [("f32", 8), ("f32", 9), ("f32", 63), ("f32", 127), ("f32", 128), ("f32", 130), ("f32", 1025),
                                       ("f32", 2500), ("bf16", 32), ("bf16", 96), ("bf16", 384), ("bf16", 768),
                                       ("bf16", 1024), ("bf16", 1056), ("bf16", 4096)])
 def test_widths(dtype, d):

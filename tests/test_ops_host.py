@@ -171,6 +171,8 @@ def test_balance_rejects_bad_calls(L):
         assert balance(L, **kw) == _lib.EINVAL, kw
     assert balance(L, cfg=dict(CFG, n_experts=0)) == _lib.EINVAL
     assert balance(L, cfg=dict(CFG, n_experts=65)) == _lib.EUNSUPPORTED
+    narrow = dict(CFG, dtype="f32", d_model=ops.BALANCE_MIN_D - 1)
+    assert balance(L, cfg=narrow) == balance(L, cfg=narrow, dX=None, dX_in=None) == _lib.EUNSUPPORTED
     size = ops.balance_loss_workspace_size(CFG, {})
     assert balance(L, nbytes=size - 1) == _lib.EWORKSPACE
     assert balance(L, ws=None) == _lib.EWORKSPACE
