@@ -48,6 +48,14 @@ __device__ __forceinline__ double wave_sum(double v) {
     return v;
 }
 
+// Sum over eight lanes side by side, in all of them.
+__device__ __forceinline__ float eight_sum(float v) {
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xf, 0xf, true));    // quad_perm [1,0,3,2]
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xf, 0xf, true));    // quad_perm [2,3,0,1]
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xf, 0xf, true));   // mirrored eight
+    return v;
+}
+
 // A group's sums, lane j those of expert j: its counts, L_s and slopes.
 __device__ __forceinline__ void balance_finish_group(const BalanceParams& p, int64_t g, double mass, int64_t load,
                                                      int64_t shared, int64_t tokens) {
@@ -255,18 +263,19 @@ __device__ __forceinline__ void balance_mean(const BalanceParams& p) {
 }
 __global__ __launch_bounds__(1024) void balance_mean_kernel(BalanceParams p) { balance_mean(p); }
 
-// The gradients of 16 steps tokens per workgroup. Its waves hold 16 NC columns
-// each, lane l the NC consecutive ones from 16-lane column l % 16 on, so that one
-// load gives a lane its operand of NC products (product i stands for every NC-th
-// column): for v_mfma_f32_16x16x4_f32, X[t + l / 16] is the right operand of
-// dl^T X and W_j the one of dl W, whose sums dX_in is added to. The router's rows
-// and the sums of dl^T X stay in registers. The next 16 tokens' rows are loaded
-// while the current ones are multiplied. dl of 64 tokens at a time is formed by
-// all waves in LDS (zeros for padded tokens, whose rows of X are not used).
-// NC = 8 up to 32 experts, 4 past that: the registers then hold two waves per
-// SIMD.
-constexpr int kBalTile = 64;
-
+// The gradients of `steps` 16-token steps per workgroup. Its waves hold 16 NC
+// columns each, lane l the NC consecutive ones from 16-lane column l % 16 on, so
+// that one load gives a lane its operand of NC products (product i stands for
+// every NC-th column): for v_mfma_f32_16x16x4_f32, X[t + l / 16] is the right
+// operand of dl^T X and W_j the one of dl W, whose sums dX_in is added to. The
+// router's rows and the sums of dl^T X stay in registers. The next 16 tokens'
+// rows are loaded while the current ones are multiplied.
+//
+// dl is formed in LDS a tile of 8 tokens per wave ahead (the waves are even in
+// number, so a tile is whole steps), eight lanes per token: a wave loads its
+// tokens' entries when the tile before begins, the slopes of their experts after
+// its first step, and writes dl behind its last; one barrier per tile. Padded
+// tokens have dl = 0, and their rows of X are not used.
 template <class T, int NC>
 struct BalRow {
     typedef T mem __attribute__((ext_vector_type(NC), aligned(sizeof(T))));
@@ -274,11 +283,17 @@ struct BalRow {
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(u16 v) { return bf2f(v); }
 
+template <int KT>
+struct BalEntries {
+    static constexpr int M = 2 * KT;   // entries per lane: ranks sub + 8 m
+    int e[M];                          // expert, 0: none
+    float v[M], a[M];                  // affinity, slope
+};
+
 template <class T, int KT, int NC>
 __global__ __launch_bounds__(512, 2) void balance_grad_kernel(BalanceParams p) {
     constexpr int KP = 16 * KT, LD = KP + 4;   // LDS row: the 16 rows' reads of 4 neighbours meet no bank twice
-    __shared__ float dls[kBalTile * LD];
-    __shared__ float means[8][kBalTile];
+    extern __shared__ float dls[];             // [2][tile][LD]
     if ((int)blockIdx.x == p.parts) {   // one workgroup more than the tokens need: the groups' mean
         if (blockIdx.y == 0) balance_mean(p);
         return;
@@ -340,45 +355,65 @@ __global__ __launch_bounds__(512, 2) void balance_grad_kernel(BalanceParams p) {
     for (int r = 0; r < 4; ++r) s[r] = f_raw{};
     load_x(first);
     load_s(first);
-    for (int64_t tb = first; tb < end; tb += kBalTile) {
-        // dl of this tile's tokens (lane: token), the entries dealt to the waves
-        const int64_t t = tb + lane;
-        const bool ok = t < end && (p.valid == nullptr || p.valid[t] != 0);
-        const uint64_t real = ballot(ok);
-        __syncthreads();   // the last tile's dl is used up
-        for (int i = threadIdx.x; i < kBalTile * LD; i += blockDim.x) dls[i] = 0.f;
-        const float* const slope = p.slope + (ok ? t / p.group : 0) * K;
-        const int* const ids = p.eids + (size_t)(ok ? t : first) * K;
-        const float* const wts = p.wts + (size_t)(ok ? t : first) * K;
-        float m = 0.f;
-        for (int i = w; i < K; i += nw) {
-            const int e = ids[i];
-            const float v = wts[i];
-            if (ok && e >= 1 && e <= K) m = fmaf(v, slope[e - 1], m);
+
+    const int tile = 8 * nw, sub = lane & 7, mine = 8 * w + (lane >> 3);   // this lane's token of a tile
+    uint32_t* const used = reinterpret_cast<uint32_t*>(dls + 2 * tile * LD);   // [2][tile]: tokens that are real
+    BalEntries<KT> en;
+    bool real;
+    auto fetch = [&](int64_t tb) {
+        const int64_t t = tb + mine;
+        real = t < end && (p.valid == nullptr || p.valid[t < end ? t : first] != 0);
+#pragma unroll
+        for (int m = 0; m < BalEntries<KT>::M; ++m) {
+            const int i = sub + 8 * m;
+            const bool on = real && i < K;
+            const size_t at = on ? (size_t)t * K + i : 0;
+            const int e = p.eids[at];
+            en.v[m] = p.wts[at];
+            en.e[m] = on && e >= 1 && e <= K ? e : 0;
         }
-        means[w][lane] = m;
-        __syncthreads();
-        m = 0.f;
-        for (int i = 0; i < nw; ++i) m += means[i][lane];
-        for (int i = w; i < K; i += nw) {
-            const int e = ids[i];
-            const float v = wts[i];
-            if (ok && e >= 1 && e <= K) dls[lane * LD + e - 1] = v * (slope[e - 1] - m);
-        }
-        __syncthreads();
-        for (int64_t t16 = tb; t16 < end && t16 < tb + kBalTile; t16 += 16) {
-            const int in_tile = (int)(t16 - tb);
-            const uint32_t mask = (uint32_t)(real >> in_tile) & 0xffffu;
-            const bool more = t16 + 16 < end;
+    };
+    auto slopes = [&](int64_t tb) {
+        const int64_t t = tb + mine;
+        const size_t row = p.groups > 1 && t < end ? (size_t)((uint32_t)t / (uint32_t)p.group) * K : 0;
+#pragma unroll
+        for (int m = 0; m < BalEntries<KT>::M; ++m) en.a[m] = p.slope[row + max(en.e[m], 1) - 1];
+    };
+    auto write = [&](int b) {
+        float s = 0.f;
+#pragma unroll
+        for (int m = 0; m < BalEntries<KT>::M; ++m) s = en.e[m] ? fmaf(en.v[m], en.a[m], s) : s;
+        s = eight_sum(s);
+        float* const row = dls + (b * tile + mine) * LD;
+        // zeros first (a wave's LDS writes land in order): tokens without the expert, the columns past K
+#pragma unroll
+        for (int m = 0; m < BalEntries<KT>::M; ++m) row[sub + 8 * m] = 0.f;
+#pragma unroll
+        for (int m = 0; m < BalEntries<KT>::M; ++m)
+            if (en.e[m]) row[en.e[m] - 1] = en.v[m] * (en.a[m] - s);
+        if (sub == 0) used[b * tile + mine] = real ? 1u : 0u;
+    };
+    fetch(first);
+    slopes(first);
+    write(0);
+    lds_barrier();
+    const bool check = p.valid != nullptr;
+    int buf = 0;
+    for (int64_t tb = first; tb < end; tb += tile) {
+        const bool ahead = tb + tile < end;
+        if (ahead) fetch(tb + tile);
+        for (int64_t t16 = tb; t16 < end && t16 < tb + tile; t16 += 16) {
+            const int in_tile = buf * tile + (int)(t16 - tb);
             const float* const dl = dls + in_tile * LD;
+            const bool more = t16 + 16 < end;
             if (p.dW != nullptr) {
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     float b[NC];
 #pragma unroll
                     for (int i = 0; i < NC; ++i) b[i] = to_f32(x[q][i]);
-                    if (mask != 0xffffu) {
-                        const bool on = mask >> (4 * q + lq) & 1;
+                    if (check || t16 + 16 > end) {
+                        const bool on = used[in_tile + 4 * q + lq] != 0;
 #pragma unroll
                         for (int i = 0; i < NC; ++i) b[i] = on ? b[i] : 0.f;
                     }
@@ -419,7 +454,11 @@ __global__ __launch_bounds__(512, 2) void balance_grad_kernel(BalanceParams p) {
                             if (i >= own) reinterpret_cast<float*>(out)[i] = v[r][i];
                 }
             }
+            if (ahead && t16 == tb) slopes(tb + tile);
         }
+        buf ^= 1;
+        if (ahead) write(buf);
+        lds_barrier();
     }
     if (p.dW == nullptr) return;
 #pragma unroll

@@ -348,11 +348,12 @@ int32_t check_balance(const unif_moe_config* c, const unif_moe_balance* b) {
 // Token ranges of the gradient: as many workgroups as run at once, two or more per
 // compute unit, so that the partial sums are few.
 constexpr int kBalParts = 512;
+constexpr int kBalNC = 4;   // columns per lane
 constexpr int kBalOnePiece = 1024, kBalPiece = 256;
 
 struct BalanceShape {
     int group, groups, pieces, piece, waves;   // count
-    int nc, cols, slabs, parts, steps;         // gradient
+    int cols, slabs, parts, steps;             // gradient
 };
 BalanceShape balance_shape(const unif_moe_config* c, const unif_moe_balance* b) {
     BalanceShape s;
@@ -363,11 +364,10 @@ BalanceShape balance_shape(const unif_moe_config* c, const unif_moe_balance* b) 
     s.piece = longest <= kBalOnePiece ? longest : kBalPiece;
     s.pieces = ceil_div(longest, s.piece);
     s.waves = std::min(kBalWaves, ceil_div(s.piece, 64));
-    // Columns per lane; waves of 16 lanes' columns, at most 8 per workgroup.
-    s.nc = c->n_experts <= 32 ? 8 : 4;
-    const int waves = ceil_div(c->d_model, 16 * s.nc);
+    // waves of 16 lanes' columns, an even number of at most 8 per workgroup
+    const int waves = ceil_div(c->d_model, 16 * kBalNC);
     s.slabs = ceil_div(waves, 8);
-    s.cols = ceil_div(waves, s.slabs);
+    s.cols = ceil_div(ceil_div(waves, s.slabs), 2) * 2;
     // Token ranges of whole 16-token steps.
     const int steps = ceil_div(N, 16);
     s.steps = ceil_div(steps, kBalParts);
@@ -392,15 +392,19 @@ BalancePlan plan_balance(const unif_moe_config* c, const unif_moe_balance* b) {
     return p;
 }
 
-template <class T>
+template <class T, int KT>
 void launch_balance_grad(const BalanceShape& s, const BalanceParams& p, unsigned extra, hipStream_t st) {
     const dim3 grid((unsigned)s.parts + extra, (unsigned)s.slabs);
-    const unsigned threads = (unsigned)s.cols * kWave;
+    const size_t tile = 8 * (size_t)s.cols, lds = 2 * tile * (16 * KT + 4 + 1) * sizeof(float);
+    balance_grad_kernel<T, KT, kBalNC><<<grid, (unsigned)s.cols * kWave, lds, st>>>(p);
+}
+template <class T>
+void launch_balance_grad(const BalanceShape& s, const BalanceParams& p, unsigned extra, hipStream_t st) {
     switch (ceil_div(p.K, 16)) {
-        case 1: balance_grad_kernel<T, 1, 8><<<grid, threads, 0, st>>>(p); break;
-        case 2: balance_grad_kernel<T, 2, 8><<<grid, threads, 0, st>>>(p); break;
-        case 3: balance_grad_kernel<T, 3, 4><<<grid, threads, 0, st>>>(p); break;
-        default: balance_grad_kernel<T, 4, 4><<<grid, threads, 0, st>>>(p); break;
+        case 1: return launch_balance_grad<T, 1>(s, p, extra, st);
+        case 2: return launch_balance_grad<T, 2>(s, p, extra, st);
+        case 3: return launch_balance_grad<T, 3>(s, p, extra, st);
+        default: return launch_balance_grad<T, 4>(s, p, extra, st);
     }
 }
 
