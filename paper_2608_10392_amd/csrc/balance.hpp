@@ -80,7 +80,7 @@ __device__ __forceinline__ void balance_finish_group(const BalanceParams& p, int
 // expert order in LDS (selected experts with the sign bit set), then lane j +
 // w h adds expert j's entries of the h-th of 64 / w runs of tokens, w the
 // experts rounded up to a power of two. A group of one piece is finished here.
-constexpr int kBalWaves = 4;
+constexpr int kBalWaves = 4, kBalBatch = 16;
 __host__ __device__ __forceinline__ int balance_wave_words(int K) { return 64 * (K | 1) + 2 * 64; }
 
 __global__ __launch_bounds__(kWave* kBalWaves) void balance_count_kernel(BalanceParams p) {
@@ -100,35 +100,42 @@ __global__ __launch_bounds__(kWave* kBalWaves) void balance_count_kernel(Balance
     double mass = 0.0;
     int load = 0, shared = 0, tokens = 0;
     for (int64_t tb = t0 + 64 * w; tb < t1; tb += 64 * nw) {
-        const int64_t t = tb + lane;
-        const bool ok = t < t1 && (p.valid == nullptr || p.valid[t] != 0);
-        const int b = ok && p.blocks ? p.nsh[t] : 0;
+        // all of the tile's loads first, as far as the registers go: they come
+        // from HBM, and a tile is short
+        const int entries = (int)(t1 - tb < 64 ? t1 - tb : 64) * K;
+        const int* const ids = p.eids + (size_t)tb * K;
+        const float* const wts = p.wts + (size_t)tb * K;
+        int e[kBalBatch];
+        float v[kBalBatch];
+        auto fetch = [&](int i0) {
+#pragma unroll
+            for (int c = 0; c < kBalBatch; ++c) {
+                const int i = min(i0 + c * kWave, entries - 1);   // past the last entry: read and not used
+                e[c] = ids[i];
+                v[c] = wts[i];
+            }
+        };
+        fetch(lane);
+        const int64_t t = tb + lane, tc = t < t1 ? t : t1 - 1;
+        const int nres = p.nres[tc], b = p.blocks ? p.nsh[tc] : 0;
+        const bool ok = (p.valid == nullptr || p.valid[tc] != 0) && t < t1;
+        for (int i = lane; i < 64 * ld; i += kWave) tile[i] = 0.f;
         unit[lane] = p.blocks ? p.B - b : 1;
-        chosen[lane] = ok ? min(p.nres[t], K) : -1;
+        chosen[lane] = ok ? min(nres, K) : -1;
         if (ok) {
             shared += p.blocks ? b : 1;
             ++tokens;
         }
-        for (int i = lane; i < 64 * ld; i += kWave) tile[i] = 0.f;
         wait_lgkmcnt0();
         __builtin_amdgcn_wave_barrier();
-        const int entries = (int)(t1 - tb < 64 ? t1 - tb : 64) * K;
-        const int* const ids = p.eids + (size_t)tb * K;
-        const float* const wts = p.wts + (size_t)tb * K;
         int q = lane / K, r = lane - q * K;         // token and rank of entry `lane`
         const int dq = kWave / K, dr = kWave - dq * K;
-        for (int i0 = lane; i0 < entries; i0 += 8 * kWave) {
-            int e[8];
-            float v[8];
+        for (int i0 = lane; i0 < entries; i0 += kBalBatch * kWave) {
+            if (i0 != lane) fetch(i0);
 #pragma unroll
-            for (int c = 0; c < 8; ++c) {
-                const int i = i0 + c * kWave;
-                e[c] = i < entries ? ids[i] : 0;
-                v[c] = i < entries ? wts[i] : 0.f;
-            }
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {
-                if (e[c] >= 1 && e[c] <= K && chosen[q] >= 0)
+            for (int c = 0; c < kBalBatch; ++c) {
+                const bool on = i0 + c * kWave < entries;
+                if (on && e[c] >= 1 && e[c] <= K && chosen[q] >= 0)
                     tile[q * ld + e[c] - 1] =
                         __uint_as_float((__float_as_uint(v[c]) & 0x7fffffffu) | (r < chosen[q] ? 0x80000000u : 0u));
                 q += dq;
@@ -144,6 +151,7 @@ __global__ __launch_bounds__(kWave* kBalWaves) void balance_count_kernel(Balance
         __builtin_amdgcn_wave_barrier();
         if (j < K) {
             float m = 0.f;
+#pragma unroll 8
             for (int i = 0; i < run; ++i) {
                 const uint32_t v = __float_as_uint(tile[(h * run + i) * ld + j]);
                 m += __uint_as_float(v & 0x7fffffffu);

@@ -345,9 +345,6 @@ int32_t check_balance(const unif_moe_config* c, const unif_moe_balance* b) {
 
 // Groups of up to this many tokens are one workgroup's in the count, which then
 // finishes them; longer ones are counted in pieces of kBalPiece.
-// Token ranges of the gradient: as many workgroups as run at once, two or more per
-// compute unit, so that the partial sums are few.
-constexpr int kBalParts = 512;
 constexpr int kBalNC = 4;   // columns per lane
 constexpr int kBalOnePiece = 1024, kBalPiece = 256;
 
@@ -355,7 +352,7 @@ struct BalanceShape {
     int group, groups, pieces, piece, waves;   // count
     int cols, slabs, parts, steps;             // gradient
 };
-BalanceShape balance_shape(const unif_moe_config* c, const unif_moe_balance* b) {
+BalanceShape balance_shape(const unif_moe_config* c, const unif_moe_balance* b, int cus) {
     BalanceShape s;
     const int N = std::max(c->n_tokens, 1);
     s.group = b->tokens_per_group > 0 ? b->tokens_per_group : N;
@@ -368,9 +365,14 @@ BalanceShape balance_shape(const unif_moe_config* c, const unif_moe_balance* b) 
     const int waves = ceil_div(c->d_model, 16 * kBalNC);
     s.slabs = ceil_div(waves, 8);
     s.cols = ceil_div(ceil_div(waves, s.slabs), 2) * 2;
-    // Token ranges of whole 16-token steps.
-    const int steps = ceil_div(N, 16);
-    s.steps = ceil_div(steps, kBalParts);
+    // Token ranges of whole 16-token steps, for one workgroup per compute unit
+    // (eight waves, where a row takes fewer): more, of which some run in a second
+    // round, cost more than the last ones' idle units, and their partial sums more
+    // traffic. 131,072 x 1,024, K = 32 (two slabs): 64 ranges 545 us, 128 328, 170
+    // 460, 256 372, 512 387; 50,432 x 768, K = 16: 64 184, 128 125, 170 156, 256
+    // 129, 512 138; 4,096 x 768, K = 8: 64 27, 128 23, 256 27.
+    const int steps = ceil_div(N, 16), ranges = std::max(1, cus * (8 / s.cols) / s.slabs);
+    s.steps = ceil_div(steps, ranges);
     s.parts = ceil_div(steps, s.steps);
     return s;
 }
@@ -379,7 +381,7 @@ struct BalancePlan {
     size_t mass, load, slope, gloss, part, total;
 };
 BalancePlan plan_balance(const unif_moe_config* c, const unif_moe_balance* b) {
-    const BalanceShape s = balance_shape(c, b);
+    const BalanceShape s = balance_shape(c, b, kMaxCus);
     const size_t K = c->n_experts, units = s.pieces > 1 ? (size_t)s.groups * s.pieces : 0;
     Carver cv;
     BalancePlan p;
@@ -439,7 +441,7 @@ int32_t unif_moe_balance_loss(const unif_moe_config* cfg, const unif_moe_balance
         if (!aligned_to(q, 4)) return UNIF_EINVAL;
     const BalancePlan plan = plan_balance(cfg, bal);
     if (workspace == nullptr || workspace_bytes < plan.total) return UNIF_EWORKSPACE;
-    const BalanceShape sh = balance_shape(cfg, bal);
+    const BalanceShape sh = balance_shape(cfg, bal, std::min(cu_count(), kMaxCus));
     const size_t nd = (size_t)N * d, wb = 4 * (size_t)(K + 1) * d;
     static const unif_moe_routing no_record{};
     const unif_moe_routing& rec = N > 0 ? *record : no_record;
