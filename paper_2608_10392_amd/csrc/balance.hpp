@@ -33,8 +33,8 @@ struct BalanceParams {
     float* dW;
     float* loss;
     int64_t* counts;       // [groups, K+1]
-    double* mass;          // [groups, pieces, K] sums of affinities
-    int64_t* load;         // [groups, pieces, K+2]: loads, the shared expert's, valid tokens
+    uint64_t* sums;        // [groups, pieces, 2 K + 2]: a piece's sums of affinities (fp64), loads, the shared
+                           // expert's load and valid tokens (int64)
     float* slope;          // [groups, K]: a_sj
     double* gloss;         // [groups]: L_s
     float* part;           // [parts][K][d]: partial dl^T X
@@ -192,66 +192,61 @@ __global__ __launch_bounds__(kWave* kBalWaves) void balance_count_kernel(Balance
         balance_finish_group(p, g, m, l, s, n);
         return;
     }
+    uint64_t* const out = p.sums + u * (2 * K + 2);
     if (lane < K) {
-        p.mass[u * K + lane] = m;
-        p.load[u * (K + 2) + lane] = l;
+        out[lane] = __builtin_bit_cast(uint64_t, m);
+        out[K + lane] = (uint64_t)l;
     }
     if (lane == 0) {
-        p.load[u * (K + 2) + K] = s;
-        p.load[u * (K + 2) + K + 1] = n;
+        out[2 * K] = (uint64_t)s;
+        out[2 * K + 1] = (uint64_t)n;
     }
 }
 
-// One workgroup per group of several pieces: each wave adds a stretch of them.
-constexpr int kBalGroupWaves = 16;
-__global__ __launch_bounds__(kWave* kBalGroupWaves) void balance_group_kernel(BalanceParams p) {
-    __shared__ double masses[kBalGroupWaves][kWave];
-    __shared__ int64_t loads[kBalGroupWaves][kWave + 2];
+// One workgroup per group of several pieces: a thread per word of a piece's sums
+// and stretch of the pieces, the stretches added in order.
+constexpr int kBalGroupThreads = 1024, kBalStretches = 32;
+__global__ __launch_bounds__(kBalGroupThreads) void balance_group_kernel(BalanceParams p) {
+    __shared__ uint64_t stretch[kBalGroupThreads];
+    __shared__ uint64_t total[2 * kWave + 2];
     const int64_t g = (int64_t)flat_block();
     if (g >= p.groups) return;
-    const int lane = lane_id(), w = (int)threadIdx.x >> 6, K = p.K;
-    const int q0 = (int)((int64_t)w * p.pieces / kBalGroupWaves), q1 = (int)((int64_t)(w + 1) * p.pieces / kBalGroupWaves);
-    double mass = 0.0;
-    int64_t load = 0, shared = 0, tokens = 0;
-    for (int q = q0; q < q1; q += 8) {
-        double m[8];
-        int64_t l[8], s[8], n[8];
+    const int K = p.K, words = 2 * K + 2, wide = 1 << (32 - __builtin_clz(words - 1));
+    const int n = min(kBalGroupThreads / wide, kBalStretches), h = (int)threadIdx.x / wide, c = (int)threadIdx.x % wide;
+    if (h < n && c < words) {
+        const int q0 = (int)((int64_t)h * p.pieces / n), q1 = (int)((int64_t)(h + 1) * p.pieces / n);
+        const uint64_t* const src = p.sums + g * p.pieces * words + c;
+        double m = 0.0;
+        uint64_t l = 0;
+        for (int q = q0; q < q1; q += 16) {
+            uint64_t v[16];
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            const int64_t u = g * p.pieces + min(q + c, q1 - 1);
-            m[c] = p.mass[u * K + min(lane, K - 1)];
-            l[c] = p.load[u * (K + 2) + min(lane, K - 1)];
-            s[c] = p.load[u * (K + 2) + K];
-            n[c] = p.load[u * (K + 2) + K + 1];
-        }
+            for (int i = 0; i < 16; ++i) v[i] = src[(size_t)min(q + i, q1 - 1) * words];
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            if (q + c >= q1) continue;
-            mass += m[c];
-            load += l[c];
-            shared += s[c];
-            tokens += n[c];
+            for (int i = 0; i < 16; ++i) {
+                if (q + i >= q1) continue;
+                m += __builtin_bit_cast(double, v[i]);
+                l += v[i];
+            }
         }
-    }
-    masses[w][lane] = mass;
-    loads[w][lane] = load;
-    if (lane == 0) {
-        loads[w][kWave] = shared;
-        loads[w][kWave + 1] = tokens;
+        stretch[threadIdx.x] = c < K ? __builtin_bit_cast(uint64_t, m) : l;
     }
     __syncthreads();
-    if (w != 0) return;
-    mass = 0.0;
-    load = shared = tokens = 0;
-    for (int i = 0; i < kBalGroupWaves; ++i) {
-        if (lane < K) {
-            mass += masses[i][lane];
-            load += loads[i][lane];
+    if ((int)threadIdx.x < words) {
+        double m = 0.0;
+        uint64_t l = 0;
+        for (int i = 0; i < n; ++i) {
+            m += __builtin_bit_cast(double, stretch[i * wide + threadIdx.x]);
+            l += stretch[i * wide + threadIdx.x];
         }
-        shared += loads[i][kWave];
-        tokens += loads[i][kWave + 1];
+        total[threadIdx.x] = (int)threadIdx.x < K ? __builtin_bit_cast(uint64_t, m) : l;
     }
-    balance_finish_group(p, g, mass, load, shared, tokens);
+    __syncthreads();
+    if (threadIdx.x >= kWave) return;
+    const int j = min((int)threadIdx.x, K - 1);
+    const bool on = (int)threadIdx.x < K;
+    balance_finish_group(p, g, on ? __builtin_bit_cast(double, total[j]) : 0.0, on ? (int64_t)total[K + j] : 0,
+                         (int64_t)total[2 * K], (int64_t)total[2 * K + 1]);
 }
 
 // *loss = the groups' mean: strided partial sums, a wave's by a butterfly, the
@@ -291,6 +286,10 @@ struct BalRow {
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(u16 v) { return bf2f(v); }
 
+// Waves that a compute unit holds, by their registers (two or three per SIMD), and
+// the most of a workgroup.
+__host__ __device__ constexpr int balance_waves(int K) { return K <= 16 ? 12 : 8; }
+
 template <int KT>
 struct BalEntries {
     static constexpr int M = 2 * KT;   // entries per lane: ranks sub + 8 m
@@ -299,7 +298,7 @@ struct BalEntries {
 };
 
 template <class T, int KT, int NC>
-__global__ __launch_bounds__(512, 2) void balance_grad_kernel(BalanceParams p) {
+__global__ __launch_bounds__(balance_waves(16 * KT) * kWave, balance_waves(16 * KT) / 4) void balance_grad_kernel(BalanceParams p) {
     constexpr int KP = 16 * KT, LD = KP + 4;   // LDS row: the 16 rows' reads of 4 neighbours meet no bank twice
     extern __shared__ float dls[];             // [2][tile][LD]
     if ((int)blockIdx.x == p.parts) {   // one workgroup more than the tokens need: the groups' mean

@@ -361,32 +361,31 @@ BalanceShape balance_shape(const unif_moe_config* c, const unif_moe_balance* b, 
     s.piece = longest <= kBalOnePiece ? longest : kBalPiece;
     s.pieces = ceil_div(longest, s.piece);
     s.waves = std::min(kBalWaves, ceil_div(s.piece, 64));
-    // waves of 16 lanes' columns, an even number of at most 8 per workgroup
+    // waves of 16 lanes' columns, an even number per workgroup
+    const int most = balance_waves(c->n_experts);
     const int waves = ceil_div(c->d_model, 16 * kBalNC);
-    s.slabs = ceil_div(waves, 8);
+    s.slabs = ceil_div(waves, most);
     s.cols = ceil_div(ceil_div(waves, s.slabs), 2) * 2;
-    // Token ranges of whole 16-token steps, for one workgroup per compute unit
-    // (eight waves, where a row takes fewer): more, of which some run in a second
+    // Token ranges of whole 16-token steps, for the workgroups that run at once: more, of which some run in a second
     // round, cost more than the last ones' idle units, and their partial sums more
     // traffic. 131,072 x 1,024, K = 32 (two slabs): 64 ranges 545 us, 128 328, 170
     // 460, 256 372, 512 387; 50,432 x 768, K = 16: 64 184, 128 125, 170 156, 256
     // 129, 512 138; 4,096 x 768, K = 8: 64 27, 128 23, 256 27.
-    const int steps = ceil_div(N, 16), ranges = std::max(1, cus * (8 / s.cols) / s.slabs);
+    const int steps = ceil_div(N, 16), ranges = std::max(1, cus * (most / s.cols) / s.slabs);
     s.steps = ceil_div(steps, ranges);
     s.parts = ceil_div(steps, s.steps);
     return s;
 }
 
 struct BalancePlan {
-    size_t mass, load, slope, gloss, part, total;
+    size_t sums, slope, gloss, part, total;
 };
 BalancePlan plan_balance(const unif_moe_config* c, const unif_moe_balance* b) {
     const BalanceShape s = balance_shape(c, b, kMaxCus);
     const size_t K = c->n_experts, units = s.pieces > 1 ? (size_t)s.groups * s.pieces : 0;
     Carver cv;
     BalancePlan p;
-    p.mass = cv.take(8 * units * K);
-    p.load = cv.take(8 * units * (K + 2));
+    p.sums = cv.take(8 * units * (2 * K + 2));
     p.slope = cv.take(4 * s.groups * K);
     p.gloss = cv.take(8 * (size_t)s.groups);
     p.part = cv.take(4 * (size_t)s.parts * K * c->d_model);
@@ -478,8 +477,7 @@ int32_t unif_moe_balance_loss(const unif_moe_config* cfg, const unif_moe_balance
     p.dW = dW_router;
     p.loss = loss;
     p.counts = counts;
-    p.mass = reinterpret_cast<double*>(ws + plan.mass);
-    p.load = reinterpret_cast<int64_t*>(ws + plan.load);
+    p.sums = reinterpret_cast<uint64_t*>(ws + plan.sums);
     p.slope = reinterpret_cast<float*>(ws + plan.slope);
     p.gloss = reinterpret_cast<double*>(ws + plan.gloss);
     p.part = reinterpret_cast<float*>(ws + plan.part);
@@ -494,7 +492,7 @@ int32_t unif_moe_balance_loss(const unif_moe_config* cfg, const unif_moe_balance
         balance_count_kernel<<<flat_grid((size_t)sh.groups * sh.pieces), (unsigned)sh.waves * kWave, lds, st>>>(p);
         UNIF_LAUNCH_CHECK();
         if (sh.pieces > 1) {
-            balance_group_kernel<<<flat_grid((size_t)sh.groups), kWave * kBalGroupWaves, 0, st>>>(p);
+            balance_group_kernel<<<flat_grid((size_t)sh.groups), kBalGroupThreads, 0, st>>>(p);
             UNIF_LAUNCH_CHECK();
         }
     }
