@@ -76,20 +76,24 @@ struct RowShape {
     int lpr, chunks, threads, rows, blocks;
     int teams() const { return lpr == 0 ? blocks : blocks * (threads / lpr); }
 };
-// Rows of up to 1,024 columns are a part of a wave's, 3 or 4 chunks of E columns
-// per lane, the fewer that cover the row; wider ones take a workgroup.
+// Rows of up to 1,024 columns are a part of a wave's, 2 or 3 chunks of E columns
+// per lane (a whole wave's also 4), the fewest columns that cover the row, more
+// lanes rather than more chunks: 2 chunks against 4 on half the lanes, 200,000 x
+// 128 bf16 42 us and 49, 400,000 x 64 45 and 59, 60,000 x 512 50 and 53; 3 chunks
+// against 2 on twice the lanes for 50,432 x 384's gradient: 67 and 79. Wider rows
+// take a workgroup, 2 chunks per lane.
 RowShape narrow_shape(int d, int threads) {
     RowShape s{};
     s.lpr = 8;
-    while (s.lpr < kWave && s.lpr * 4 * E < d) s.lpr *= 2;
-    s.chunks = s.lpr * 3 * E >= d ? 3 : 4;
+    while (s.lpr < kWave && s.lpr * 3 * E < d) s.lpr *= 2;
+    s.chunks = s.lpr * 2 * E >= d ? 2 : s.lpr * 3 * E >= d ? 3 : 4;
     s.threads = threads;
     return s;
 }
-RowShape wide_shape(int d, int chunks) {
+RowShape wide_shape(int d) {
     RowShape s{};
-    s.chunks = chunks;
-    s.threads = ceil_div(d, kWave * chunks * E) * kWave;
+    s.chunks = 2;
+    s.threads = ceil_div(d, kWave * 2 * E) * kWave;
     return s;
 }
 // The tokens dealt to at most `waves` waves per compute unit.
@@ -102,54 +106,51 @@ RowShape cover(RowShape s, int N, int cus, int waves) {
 }
 
 // Calls f(chunks, lanes per row) for a launch's shape.
-template <int CH, int Wide, class F>
-void with_lanes(const RowShape& s, F f) {
-    const std::integral_constant<int, CH> ch;
-    switch (s.lpr) {
-        case 8: return f(ch, std::integral_constant<int, 8>());
-        case 16: return f(ch, std::integral_constant<int, 16>());
-        case 32: return f(ch, std::integral_constant<int, 32>());
-        case 64: return f(ch, std::integral_constant<int, 64>());
-        default: return f(std::integral_constant<int, Wide>(), std::integral_constant<int, 0>());
-    }
+template <class F>
+void with_shape(const RowShape& s, F f) {
+    const std::integral_constant<int, 2> two;
+    const std::integral_constant<int, 3> three;
+    const std::integral_constant<int, 8> l8;
+    const std::integral_constant<int, 16> l16;
+    const std::integral_constant<int, 32> l32;
+    const std::integral_constant<int, 64> l64;
+    if (s.lpr == 0) return f(two, std::integral_constant<int, 0>());
+    if (s.chunks == 4) return f(std::integral_constant<int, 4>(), l64);
+    if (s.chunks == 3) return s.lpr == 8 ? f(three, l8) : s.lpr == 16 ? f(three, l16) : s.lpr == 32 ? f(three, l32) : f(three, l64);
+    return s.lpr == 8 ? f(two, l8) : s.lpr == 16 ? f(two, l16) : s.lpr == 32 ? f(two, l32) : f(two, l64);
 }
 
 constexpr int kNarrowD = kWave * 4 * E;
 // Forward: many more waves than run at once, so that the last ones of a launch
-// leave little of the chip idle, but fewer where a wave holds several rows and
-// the parameters' loads would weigh: 65,536 x 1,024 bf16 113.5 us with 16 waves
-// per compute unit, 111 with 32, 108.8 with 64; 200,000 x 128 46 with 16, 51 with
-// 32, 52 with 64. Wide rows in 2 chunks a lane: 16,384 x 2,048 66.6 us, in 4 77.
+// leave little of the chip idle: 65,536 x 1,024 bf16 113.5 us with 16 waves per
+// compute unit, 111 with 32, 108.8 with 64; 200,000 x 128 46.6, 44.9 and 42.5.
+// Fewer for wide rows, whose teams are few and share barriers: 8,192 x 8,192 113,
+// 116.5 and 117.5, 16,384 x 2,048 67, 63 and 66.
 RowShape forward_shape(const unif_moe_residual* r, int cus) {
-    if (r->d_model > kNarrowD) return cover(wide_shape(r->d_model, 2), r->n_tokens, cus, 32);
-    const RowShape s = narrow_shape(r->d_model, 256);
-    return cover(s, r->n_tokens, cus, std::max(16, s.lpr));
+    if (r->d_model > kNarrowD) return cover(wide_shape(r->d_model), r->n_tokens, cus, 32);
+    return cover(narrow_shape(r->d_model, 256), r->n_tokens, cus, 64);
 }
 // Backward: as many waves as run at once (two per SIMD, by their registers), so
 // that the partial rows are few: 50,432 x 768 134 us with 8 waves per compute
-// unit, 168 with 4, 158 with 24. Wide rows in 4 chunks a lane: 16,384 x 4,096
-// 183 us, in 3 247, in 2 226 to 283.
+// unit, 168 with 4, 158 with 24. Wide rows in 2 chunks a lane: 16,384 x 4,096
+// 170 us, in 3 212, in 4 184; 4,099 x 5,120 72, 78 and 79.
 RowShape backward_shape(const unif_moe_residual* r, int cus) {
-    return cover(r->d_model > kNarrowD ? wide_shape(r->d_model, 4) : narrow_shape(r->d_model, 512), r->n_tokens, cus, 8);
+    return cover(r->d_model > kNarrowD ? wide_shape(r->d_model) : narrow_shape(r->d_model, 512), r->n_tokens, cus, 8);
 }
 
 template <class S, class L>
 void launch_forward(const RowShape& s, const ResidualParams& p, hipStream_t st) {
-    const auto launch = [&](auto ch, auto lpr) {
+    with_shape(s, [&](auto ch, auto lpr) {
         residual_forward_kernel<S, L, ch.value, lpr.value><<<(unsigned)s.blocks, (unsigned)s.threads, 0, st>>>(p);
-    };
-    if (s.chunks == 3) with_lanes<3, 2>(s, launch);
-    else with_lanes<4, 2>(s, launch);
+    });
 }
 template <class S, class L, class H>
 void launch_backward(const RowShape& s, const ResidualParams& p, hipStream_t st) {
     const size_t lds = (size_t)(s.teams() / s.blocks) * 2 * p.d * sizeof(float);
-    const auto launch = [&](auto ch, auto lpr) {
+    with_shape(s, [&](auto ch, auto lpr) {
         residual_backward_kernel<S, L, H, ch.value, lpr.value>
             <<<(unsigned)s.blocks, (unsigned)s.threads, lds, st>>>(p);
-    };
-    if (s.chunks == 3) with_lanes<3, 4>(s, launch);
-    else with_lanes<4, 4>(s, launch);
+    });
 }
 
 ResidualParams residual_params(const unif_moe_residual* r, const RowShape& s) {

@@ -171,8 +171,8 @@ __device__ __forceinline__ float lanes_sum(float v) {
 }
 
 // The lanes that hold one row: LPR lanes of a wave, or (LPR = 0) all waves of
-// the workgroup, whose sums are added in order.
-constexpr int kWideWaves = 16;   // most waves of a wide team (backward: 8)
+// the workgroup.
+constexpr int kWideWaves = 16;   // most waves of a wide team
 template <int LPR>
 struct Team {
     static constexpr bool kWide = LPR == 0;
@@ -201,11 +201,10 @@ struct Team {
 #pragma unroll
                 for (int i = 0; i < NV; ++i) r[w * 4 + i] = v[i];
             lds_barrier();
+            // every 16 lanes read the waves' sums side by side
+            const int k = lane_id() & (kWideWaves - 1);
 #pragma unroll
-            for (int i = 0; i < NV; ++i) v[i] = 0.f;
-            for (int k = 0; k < nw; ++k)
-#pragma unroll
-                for (int i = 0; i < NV; ++i) v[i] += r[k * 4 + i];
+            for (int i = 0; i < NV; ++i) v[i] = lanes_sum<kWideWaves>(k < nw ? r[k * 4 + i] : 0.f);
         }
     }
 };
@@ -370,7 +369,7 @@ __global__ __launch_bounds__(LPR == 0 ? kWideWaves * kWave : 256) void residual_
 constexpr int kSumOutGamma = 0, kSumOutBeta = 1, kSumInGamma = 2, kSumInBeta = 3;
 
 template <class S, class L, class H, int CH, int LPR>
-__global__ __launch_bounds__(512) void residual_backward_kernel(ResidualParams p) {
+__global__ __launch_bounds__(LPR == 0 ? kWideWaves * kWave : 512) void residual_backward_kernel(ResidualParams p) {
     __shared__ float red[2 * kWideWaves * 4];
     extern __shared__ float sums[];   // [teams of the workgroup][2][d]
     Team<LPR> team{red, 0};
@@ -493,6 +492,7 @@ __global__ __launch_bounds__(512) void residual_backward_kernel(ResidualParams p
             const int which = first + (i >= p.d ? 1 : 0);
             if (!(p.want >> which & 1)) continue;
             float s = 0.f;
+#pragma unroll 8
             for (int t = 0; t < nteam; ++t) s += sums[(size_t)t * 2 * p.d + i];
             p.part[((size_t)which * gridDim.x + blockIdx.x) * p.d + (i >= p.d ? i - p.d : i)] = s;
         }

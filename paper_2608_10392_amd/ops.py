@@ -68,40 +68,51 @@ def _refuse(where, what):
 
 
 class _Tensors:
-    """Checks a call's tensors (all on one device) and yields their pointers."""
+    """Checks a call's tensors (all on one GPU) and yields their pointers."""
+    __slots__ = ("where", "device")
 
-    def __init__(self, where):
-        self.where, self.device = where, None
+    def __init__(self, where, device=None):
+        self.where, self.device = where, device   # device: index of the tensors' GPU
 
     def __call__(self, name, t, dtype, numel):
         if t is None:
             return None
-        if not t.is_cuda:
+        device = t.get_device()
+        if t.dtype is dtype and t.numel() == numel and device == self.device and t.is_contiguous():
+            return t.data_ptr()
+        if device < 0 or not t.is_cuda:
             _refuse(self.where, f"{name} is not on a GPU")
         if t.dtype != dtype:
             _refuse(self.where, f"{name} is {t.dtype}, not {dtype}")
         if t.numel() != numel or not t.is_contiguous():
             _refuse(self.where, f"{name} is not a contiguous tensor of {numel} elements")
-        if self.device is None:
-            self.device = t.device
-        elif t.device != self.device:
-            _refuse(self.where, f"{name} is on {t.device}, other tensors on {self.device}")
+        if self.device is not None and device != self.device:
+            _refuse(self.where, f"{name} is on GPU {device}, other tensors on GPU {self.device}")
+        self.device = device
         return t.data_ptr()
 
     def workspace(self, t):
         if t is None:
             return None, 0
-        return self("workspace", t.view(-1) if t.is_contiguous() else t, t.dtype, t.numel()), t.numel() * t.element_size()
+        return self("workspace", t, t.dtype, t.numel()), t.nbytes
 
     def call(self, fn, args, stream):
         """fn(*args, stream) with the tensors' device current."""
         import torch
-        if self.device is None or self.device.index == torch.cuda.current_device():
-            status = fn(*args, _lib._stream(stream))
+        if self.device is None or self.device == torch.cuda.current_device():
+            status = fn(*args, _stream(stream, self.device))
         else:
             with torch.cuda.device(self.device):
-                status = fn(*args, _lib._stream(stream))
-        _lib._check(status, self.where)
+                status = fn(*args, _stream(stream, self.device))
+        if status != _lib.OK:
+            _lib._check(status, self.where)
+
+
+def _stream(stream, device):
+    if stream is None and device is not None:
+        import torch
+        return torch._C._cuda_getCurrentRawStream(device)
+    return _lib._stream(stream)
 
 
 def _torch_dtype(code):
@@ -140,9 +151,7 @@ def make_residual(desc):
 
 def _residual(res, where):
     r = make_residual(res) if isinstance(res, dict) else res
-    at = _Tensors(where)
-    at.device = r.device
-    return r, at
+    return r, _Tensors(where, r.device)
 
 
 def residual_forward(res, x, f, valid, y, h, stream=None):
