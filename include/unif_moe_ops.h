@@ -55,7 +55,7 @@ typedef struct unif_moe_residual {
     int32_t tokens_per_gate; /* 0: one gate row for every token; R > 0: a gate row
                                 per R consecutive tokens (one sequence or image),
                                 ceil(N / R) rows. Unused without a gate              */
-    float   out_eps, in_eps; /* eps > 0, finite (unused for NONE)                    */
+    float   out_eps, in_eps; /* eps >= FLT_MIN, finite (unused for NONE)             */
     float   residual_scale;  /* finite; a constant, without a gradient               */
     const float* out_gamma;  /* [d] fp32 device array; NULL exactly for NONE         */
     const float* out_beta;   /* [d] or NULL (no shift); NULL for NONE                */

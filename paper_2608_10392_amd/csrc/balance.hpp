@@ -56,6 +56,13 @@ __device__ __forceinline__ float eight_sum(float v) {
     return v;
 }
 
+// LDS writes of a wave's lanes before, its reads after, in order.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // A group's sums, lane j those of expert j: its counts, L_s and slopes.
 __device__ __forceinline__ void balance_finish_group(const BalanceParams& p, int64_t g, double mass, int64_t load,
                                                      int64_t shared, int64_t tokens) {
@@ -126,8 +133,7 @@ __global__ __launch_bounds__(kWave* kBalWaves) void balance_count_kernel(Balance
             shared += p.blocks ? b : 1;
             ++tokens;
         }
-        wait_lgkmcnt0();
-        __builtin_amdgcn_wave_barrier();
+        wave_sync();
         int q = lane / K, r = lane - q * K;         // token and rank of entry `lane`
         const int dq = kWave / K, dr = kWave - dq * K;
         for (int i0 = lane; i0 < entries; i0 += kBalBatch * kWave) {
@@ -147,8 +153,7 @@ __global__ __launch_bounds__(kWave* kBalWaves) void balance_count_kernel(Balance
                 q = min(q, 63);   // past the last entry
             }
         }
-        wait_lgkmcnt0();
-        __builtin_amdgcn_wave_barrier();
+        wave_sync();
         if (j < K) {
             float m = 0.f;
 #pragma unroll 8
@@ -159,8 +164,7 @@ __global__ __launch_bounds__(kWave* kBalWaves) void balance_count_kernel(Balance
             }
             mass += (double)m;
         }
-        wait_lgkmcnt0();
-        __builtin_amdgcn_wave_barrier();
+        wave_sync();
     }
     for (int o = 32; o >= wide; o >>= 1) {
         mass += __shfl_xor(mass, o);

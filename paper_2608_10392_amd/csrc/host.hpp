@@ -79,4 +79,13 @@ inline bool record_complete(const unif_moe_routing* r) {
         if (hipGetLastError() != hipSuccess) return UNIF_EDEVICE; \
     } while (0)
 
+template <class F>
+int32_t allow_lds(F* kernel, size_t bytes) {
+    if (bytes <= 64 * 1024) return UNIF_OK;
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                            (int)bytes) != hipSuccess)
+        return UNIF_EDEVICE;
+    return UNIF_OK;
+}
+
 }  // namespace unifmoe

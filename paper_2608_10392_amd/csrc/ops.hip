@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 
@@ -46,7 +47,7 @@ bool apart(const Span (&out)[NO], const Span (&partner)[NO], const Span (&in)[NI
 bool norm_ok(int32_t norm, float eps, const float* gamma, const float* beta) {
     if (norm == UNIF_ROWNORM_NONE) return gamma == nullptr && beta == nullptr;
     if (norm != UNIF_ROWNORM_LAYER && norm != UNIF_ROWNORM_RMS) return false;
-    return eps > 0.0f && std::isfinite(eps) && gamma != nullptr;
+    return eps >= FLT_MIN && std::isfinite(eps) && gamma != nullptr;   // 1 / sqrt(eps) is formed in fp32
 }
 
 int32_t check_residual(const unif_moe_residual* r) {
@@ -70,6 +71,9 @@ int64_t gate_rows(const unif_moe_residual* r) {
 size_t gate_bytes(const unif_moe_residual* r) { return (size_t)gate_rows(r) * r->d_model * sizeof(float); }
 // Several gate rows: their gradients are sums over parts of the tokens.
 bool gate_grouped(const unif_moe_residual* r) { return r->gate != nullptr && gate_rows(r) > 1; }
+
+// LDS that the kernels declare beside what their launch asks for.
+constexpr size_t kTeamLds = 2 * kWideWaves * 4 * sizeof(float), kCountLds = kBalWaves * (kWave * 12 + 8);
 
 // Lanes per row (0: the workgroup) and the launch that covers the tokens.
 struct RowShape {
@@ -145,12 +149,16 @@ void launch_forward(const RowShape& s, const ResidualParams& p, hipStream_t st) 
     });
 }
 template <class S, class L, class H>
-void launch_backward(const RowShape& s, const ResidualParams& p, hipStream_t st) {
+int32_t launch_backward(const RowShape& s, const ResidualParams& p, hipStream_t st) {
     const size_t lds = (size_t)(s.teams() / s.blocks) * 2 * p.d * sizeof(float);
+    int32_t status = UNIF_OK;
     with_shape(s, [&](auto ch, auto lpr) {
+        status = allow_lds(residual_backward_kernel<S, L, H, ch.value, lpr.value>, lds + kTeamLds);
+        if (status != UNIF_OK) return;
         residual_backward_kernel<S, L, H, ch.value, lpr.value>
             <<<(unsigned)s.blocks, (unsigned)s.threads, lds, st>>>(p);
     });
+    return status;
 }
 
 ResidualParams residual_params(const unif_moe_residual* r, const RowShape& s) {
@@ -311,11 +319,14 @@ int32_t unif_moe_residual_backward(const unif_moe_residual* res, const void* y, 
     p.want = (gr.out_gamma != nullptr || one_gate ? 1 << kSumOutGamma : 0) |
              (gr.out_beta != nullptr || one_gate ? 1 << kSumOutBeta : 0) |
              (gr.in_gamma != nullptr ? 1 << kSumInGamma : 0) | (gr.in_beta != nullptr ? 1 << kSumInBeta : 0);
-    if (res->dtype == UNIF_F32) launch_backward<float, float, float>(sh, p, st);
-    else if (res->stream_dtype == UNIF_F32 && dh_dtype == UNIF_F32) launch_backward<float, u16, float>(sh, p, st);
-    else if (res->stream_dtype == UNIF_F32) launch_backward<float, u16, u16>(sh, p, st);
-    else if (dh_dtype == UNIF_F32) launch_backward<u16, u16, float>(sh, p, st);
-    else launch_backward<u16, u16, u16>(sh, p, st);
+    int32_t status;
+    if (res->dtype == UNIF_F32) status = launch_backward<float, float, float>(sh, p, st);
+    else if (res->stream_dtype == UNIF_F32 && dh_dtype == UNIF_F32)
+        status = launch_backward<float, u16, float>(sh, p, st);
+    else if (res->stream_dtype == UNIF_F32) status = launch_backward<float, u16, u16>(sh, p, st);
+    else if (dh_dtype == UNIF_F32) status = launch_backward<u16, u16, float>(sh, p, st);
+    else status = launch_backward<u16, u16, u16>(sh, p, st);
+    if (status != UNIF_OK) return status;
     UNIF_LAUNCH_CHECK();
     if (p.want != 0 || p.dgate != nullptr) {
         const int by_wave = p.group / p.rows <= kFinishWaves;
@@ -487,9 +498,8 @@ int32_t unif_moe_balance_loss(const unif_moe_config* cfg, const unif_moe_balance
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (sh.groups > 0) {
         const size_t lds = sizeof(float) * sh.waves * (size_t)balance_wave_words(K);
-        if (lds > 64 * 1024 - 4096 && hipFuncSetAttribute(reinterpret_cast<const void*>(balance_count_kernel),
-                                                          hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
-            return UNIF_EDEVICE;
+        const int32_t status = allow_lds(balance_count_kernel, lds + kCountLds);
+        if (status != UNIF_OK) return status;
         balance_count_kernel<<<flat_grid((size_t)sh.groups * sh.pieces), (unsigned)sh.waves * kWave, lds, st>>>(p);
         UNIF_LAUNCH_CHECK();
         if (sh.pieces > 1) {

@@ -421,15 +421,6 @@ FwdPlan plan_forward(const Dims& m, size_t xn_bytes = 0) {
     return p;
 }
 
-template <class F>
-int32_t allow_lds(F* kernel, size_t bytes) {
-    if (bytes <= 64 * 1024) return UNIF_OK;
-    if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
-                            (int)bytes) != hipSuccess)
-        return UNIF_EDEVICE;
-    return UNIF_OK;
-}
-
 template <class P>
 int32_t launch_persistent(void (*kernel)(P), int grid, size_t lds, hipStream_t st, const P& prm) {
     if (allow_lds(kernel, lds) != UNIF_OK) return UNIF_EDEVICE;

@@ -35,6 +35,8 @@ class Balance(ctypes.Structure):
     _fields_ = [("tokens_per_group", ctypes.c_int32), ("unit", ctypes.c_int32), ("weight", ctypes.c_float)]
 
 
+RESIDUAL_KEYS = frozenset(k for k, _ in Residual._fields_)
+BALANCE_KEYS = frozenset(k for k, _ in Balance._fields_)
 EXPORTS = ("unif_moe_residual_forward", "unif_moe_residual_backward_workspace_size", "unif_moe_residual_backward",
            "unif_moe_balance_loss_workspace_size", "unif_moe_balance_loss")
 _LIB = None
@@ -65,6 +67,11 @@ def _refuse(where, what):
     e = UnifMoeError(EINVAL, where)
     e.args = (f"{e.args[0]}: {what}",)
     raise e
+
+
+def _known(where, desc, keys):
+    if not keys.issuperset(desc):
+        _refuse(where, f"unknown keys {sorted(set(desc) - keys)}")
 
 
 class _Tensors:
@@ -133,6 +140,7 @@ def make_residual(desc):
     in_gamma, in_beta [d] and gate [rows, d]. Calls with the same description
     can share the structure."""
     import torch
+    _known("make_residual", desc, RESIDUAL_KEYS)
     n, d = int(desc["n_tokens"]), int(desc["d_model"])
     per = int(desc.get("tokens_per_gate", 0))
     r = Residual(n_tokens=n, d_model=d, dtype=_lib.DTYPES[desc["dtype"]],
@@ -195,6 +203,7 @@ def residual_backward(res, y, f, valid, dy, dh, dx, df, grads, workspace, stream
 def make_balance(bal):
     """Balance structure from a dict: tokens_per_group (0: one group), unit
     ("tokens", "blocks"), weight (1)."""
+    _known("make_balance", bal, BALANCE_KEYS)
     return Balance(tokens_per_group=int(bal.get("tokens_per_group", 0)),
                    unit=BALANCE_UNITS[bal.get("unit", "tokens")], weight=float(bal.get("weight", 1.0)))
 

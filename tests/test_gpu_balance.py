@@ -289,3 +289,22 @@ def test_binding_refuses():
                      (dict(dX_in=c.dX_in.t().contiguous().t()), "dX_in is not a contiguous")):
         with pytest.raises(_lib.UnifMoeError, match=what):
             c.run(**kw)
+
+
+def test_offsets_past_32_bits():
+    """Tensors of more than 2^32 bytes: the last group's rows of dX are those of
+    a call of its own, with the weight of its share of the mean."""
+    per, groups, d, K = 1024, 1280, 1024, 4
+    n = per * groups
+    print(f"\n[gpu] balance: {n} x {d}", flush=True)
+    c = Case(n, d, K, dtype="bf16", per=per, weight=640.0, add=False)
+    o = c.run()
+    last = Case(per, d, K, dtype="bf16", weight=0.5, add=False)
+    last.rec, last.X, last.W = {k: v[-per:].contiguous() for k, v in c.rec.items()}, c.X[-per:], c.W
+    want = last.run()
+    assert torch.equal(o["counts"][-1:], want["counts"])
+    # the slopes' quotients may round differently: two fp32 steps of a sum of K terms' absolute values
+    err = (o["dX"][-per:] - want["dX"]).abs().max()
+    assert float(err) <= 8 * K * U * float(want["dX"].abs().max())
+    del c, o
+    torch.cuda.empty_cache()

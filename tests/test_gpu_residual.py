@@ -423,3 +423,29 @@ def test_binding_refuses(bad, what):
     with pytest.raises(_lib.UnifMoeError, match=what) as e:
         ops.residual_forward(c.res, a["x"], a["f"], None, a["y"], a["h"])
     assert e.value.status == _lib.EINVAL
+
+
+def test_offsets_past_32_bits():
+    """Tensors of more than 2^32 bytes: the last rows are those of a call of
+    their own."""
+    n, d, tail = 700_001, 1600, 33
+    print(f"\n[gpu] residual: {n} x {d}", flush=True)
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(5)
+    rnd = lambda *s: torch.randn(*s, generator=gen, device=DEV)
+    x, f = rnd(n, d), rnd(n, d).to(torch.bfloat16)
+    p = dict(in_gamma=1 + 0.2 * rnd(d), out_gamma=1 + 0.2 * rnd(d), gate=rnd(1, d))
+    desc = dict(d_model=d, dtype="bf16", stream_dtype="f32", in_norm="rms", out_norm="layer", **p)
+    got, want = [], []
+    for rows, out in ((slice(0, n), got), (slice(n - tail, n), want)):
+        xs, fs = x[rows], f[rows]
+        res = ops.make_residual(dict(desc, n_tokens=len(xs)))
+        y, h = torch.empty_like(xs), torch.empty_like(fs)
+        ops.residual_forward(res, xs, fs, None, y, h)
+        out += [y[-tail:].clone(), h[-tail:].clone()]
+        ws = _lib.alloc_workspace(ops.residual_backward_workspace_size(res), DEV)
+        ops.residual_backward(res, xs, fs, None, xs, fs, y, h, None, ws)
+        out += [y[-tail:].clone(), h[-tail:].clone()]
+        del y, h
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    torch.cuda.empty_cache()

@@ -76,7 +76,7 @@ def backward(L, r, dh_dtype=0, nbytes=1 << 29, grads=None, **kw):
 
 BAD_RESIDUALS = [
     dict(n_tokens=-1), dict(d_model=0), dict(dtype=2), dict(stream_dtype=5), dict(dtype=0, stream_dtype=1),
-    dict(out_norm=3), dict(in_norm=-1), dict(tokens_per_gate=-1), dict(out_eps=0.0), dict(in_eps=math.nan),
+    dict(out_norm=3), dict(in_norm=-1), dict(tokens_per_gate=-1), dict(out_eps=0.0), dict(in_eps=1e-39), dict(in_eps=math.nan),
     dict(out_eps=math.inf), dict(residual_scale=math.nan), dict(residual_scale=math.inf), dict(out_gamma=None),
     dict(in_gamma=None), dict(out_norm=0), dict(in_norm=0), dict(gate=A["gate"] + 2),
 ]
@@ -190,3 +190,6 @@ def test_binding_checks_tensors():
         ops.residual_forward(r, torch.zeros(4, 8), None, None, None, None)
     with pytest.raises(KeyError):
         ops.make_residual(dict(desc, in_norm="batch"))
+    for make, bad in ((ops.make_residual, dict(desc, gamma=None)), (ops.make_balance, dict(lam=0.1))):
+        with pytest.raises(_lib.UnifMoeError, match="unknown keys"):
+            make(bad)
