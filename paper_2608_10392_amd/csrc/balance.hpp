@@ -19,6 +19,7 @@ struct BalanceParams {
     int pieces;            // workgroups per group in the count
     int piece;             // tokens of a group per workgroup
     int blocks;            // loads count blocks
+    int past;              // dX is larger than the caches: stored past them
     float weight;
     const uint8_t* valid;
     const int* nsh;
@@ -458,7 +459,8 @@ __global__ __launch_bounds__(balance_waves(16 * KT) * kWave, balance_waves(16 * 
                 for (int r = 0; r < 4; ++r) {
                     if (t16 + 4 * lq + r >= end) continue;
                     char* const out = reinterpret_cast<char*>(p.dX) + (size_t)(t16 + r) * p.d * 4 + soff;
-                    if (own == 0) *reinterpret_cast<f_mem*>(out) = v[r];
+                    if (own == 0 && p.past) __builtin_nontemporal_store(v[r], reinterpret_cast<f_mem*>(out));
+                    else if (own == 0) *reinterpret_cast<f_mem*>(out) = v[r];
                     else
 #pragma unroll
                         for (int i = 0; i < NC; ++i)

@@ -129,14 +129,17 @@ struct Cols {
         }
         fix(true, v);
     }
-    template <class T>
+    template <bool PAST = false, class T>   // PAST: around the caches
     __device__ __forceinline__ void store(T* row, const float (&v)[CH][E]) const {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const typename Vec<T>::raw w = Vec<T>::pack(v[c]);
-            if ((int)col[c] + E <= d)
-                *reinterpret_cast<typename Vec<T>::mem*>(reinterpret_cast<char*>(row) + col[c] * (uint32_t)sizeof(T)) = w;
-            else
+            typename Vec<T>::mem* const out =
+                reinterpret_cast<typename Vec<T>::mem*>(reinterpret_cast<char*>(row) + col[c] * (uint32_t)sizeof(T));
+            if ((int)col[c] + E <= d) {
+                if constexpr (PAST) __builtin_nontemporal_store(w, out);
+                else *out = w;
+            } else
 #pragma unroll
                 for (int e = 0; e < E; ++e)
                     if (in(c, e)) row[col[c] + e] = w[e];
@@ -303,7 +306,8 @@ __device__ __forceinline__ void normalise_grad(Team<LPR>& team, int norm, float 
     UNIF_COLS(c, e) a[c][e] = fmaf(hat[c][e], q, fmaf(a[c][e], rstd, m));
 }
 
-template <class S, class L, int CH, int LPR>
+// PAST: the outputs are larger than the caches and stored around them.
+template <class S, class L, bool PAST, int CH, int LPR>
 __global__ __launch_bounds__(LPR == 0 ? kWideWaves * kWave : 256) void residual_forward_kernel(ResidualParams p) {
     __shared__ float red[2 * kWideWaves * 4];
     Team<LPR> team{red, 0};
@@ -344,12 +348,12 @@ __global__ __launch_bounds__(LPR == 0 ? kWideWaves * kWave : 256) void residual_
         if (p.out_norm != kNormNone) normalise<CH, LPR>(team, k, p.out_norm, p.out_eps, p.inv_d, v);
         UNIF_COLS(c, e) v[c][e] = fmaf(p.scale, u[c][e], fmaf(v[c][e], cg[c][e], cb[c][e]));
         if (!keep) UNIF_COLS(c, e) v[c][e] = 0.f;
-        if (p.y != nullptr) k.store(static_cast<S*>(p.y) + at, v);
+        if (p.y != nullptr) k.template store<PAST>(static_cast<S*>(p.y) + at, v);
         if (p.h != nullptr) {
             normalise<CH, LPR>(team, k, p.in_norm, p.in_eps, p.inv_d, v);
             UNIF_COLS(c, e) v[c][e] = fmaf(v[c][e], ig[c][e], ib[c][e]);
             if (!keep) UNIF_COLS(c, e) v[c][e] = 0.f;
-            k.store(static_cast<L*>(p.h) + at, v);
+            k.template store<PAST>(static_cast<L*>(p.h) + at, v);
         }
     }
 }
