@@ -88,7 +88,7 @@ __device__ __forceinline__ void balance_finish_group(const BalanceParams& p, int
 // expert order in LDS (selected experts with the sign bit set), then lane j +
 // w h adds expert j's entries of the h-th of 64 / w runs of tokens, w the
 // experts rounded up to a power of two. A group of one piece is finished here.
-constexpr int kBalWaves = 4, kBalBatch = 16;
+constexpr int kBalWaves = 8, kBalBatch = 16;
 __host__ __device__ __forceinline__ int balance_wave_words(int K) { return 64 * (K | 1) + 2 * 64; }
 
 __global__ __launch_bounds__(kWave* kBalWaves) void balance_count_kernel(BalanceParams p) {

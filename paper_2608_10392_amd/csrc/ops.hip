@@ -368,7 +368,7 @@ int32_t check_balance(const unif_moe_config* c, const unif_moe_balance* b) {
 // Groups of up to this many tokens are one workgroup's in the count, which then
 // finishes them; longer ones are counted in pieces of kBalPiece.
 constexpr int kBalNC = 4;   // columns per lane
-constexpr int kBalOnePiece = 1024, kBalPiece = 256;
+constexpr int kBalOnePiece = 1024, kBalPiece = 512;
 
 struct BalanceShape {
     int group, groups, pieces, piece, waves;   // count
