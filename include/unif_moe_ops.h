@@ -165,7 +165,8 @@ int32_t unif_moe_balance_loss_workspace_size(const unif_moe_config* cfg, const u
  *   dW_router_in, dW_router   [K+1, d] fp32, likewise
  * A training step calls it after unif_moe_layer_backward with the layer's
  * gradients in place. cfg is validated as for the layer; N, d, K, B and dtype
- * are read. Other overlaps of outputs with inputs or each other are rejected.
+ * are read (d <= 2^20). Other overlaps of outputs with inputs or each other are
+ * rejected.
  * Precision: p, the loads' shares and the gradients in fp32, sums over tokens
  * in fp32 within a workgroup's tokens and in fp64 past that, in a fixed order:
  * repeated calls give the same bits.

@@ -17,6 +17,9 @@ using namespace unifmoe;
 
 namespace {
 
+// Quotient rounded up; token counts may be near INT32_MAX.
+int div_up(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
 size_t elem_size(int32_t dtype) { return dtype == UNIF_BF16 ? 2 : 4; }
 
 bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
@@ -97,15 +100,15 @@ RowShape narrow_shape(int d, int threads) {
 RowShape wide_shape(int d) {
     RowShape s{};
     s.chunks = 2;
-    s.threads = ceil_div(d, kWave * 2 * E) * kWave;
+    s.threads = div_up(d, kWave * 2 * E) * kWave;
     return s;
 }
 // The tokens dealt to at most `waves` waves per compute unit.
 RowShape cover(RowShape s, int N, int cus, int waves) {
     const int per_block = s.lpr == 0 ? 1 : s.threads / s.lpr;
     const int most = cus * std::max(1, waves / (s.threads / kWave)) * per_block;
-    s.rows = std::max(1, ceil_div(N, most));
-    s.blocks = ceil_div(ceil_div(N, s.rows), per_block);
+    s.rows = std::max(1, div_up(N, most));
+    s.blocks = div_up(div_up(N, s.rows), per_block);
     return s;
 }
 
@@ -345,7 +348,7 @@ int32_t unif_moe_residual_backward(const unif_moe_residual* res, const void* y, 
                                  {gr.out_gamma, gr.out_beta, gr.in_gamma, gr.in_beta}, gr.gate};
         int64_t shared = p.dgate != nullptr ? std::min<int64_t>(sh.teams() - 1, gate_rows(res)) : 0;
         if (by_wave) shared = (shared + kFinishWaves - 1) / kFinishWaves;
-        residual_finish_kernel<<<dim3((unsigned)ceil_div(p.d, kWave), (unsigned)(4 + shared)), kFinishWaves * kWave, 0,
+        residual_finish_kernel<<<dim3((unsigned)div_up(p.d, kWave), (unsigned)(4 + shared)), kFinishWaves * kWave, 0,
                                  st>>>(fin);
         UNIF_LAUNCH_CHECK();
     }
@@ -360,7 +363,7 @@ int32_t check_balance(const unif_moe_config* c, const unif_moe_balance* b) {
     const int32_t s = check_config(c);
     if (s != UNIF_OK) return s;
     if (b == nullptr || b->tokens_per_group < 0 || !std::isfinite(b->weight)) return UNIF_EINVAL;
-    if (c->d_model > 1 << 24) return UNIF_EUNSUPPORTED;   // 32-bit offsets inside 16 rows
+    if (c->d_model > 1 << 20) return UNIF_EUNSUPPORTED;   // 32-bit offsets inside 16 rows, threads of a grid
     if (b->unit != UNIF_BALANCE_TOKENS && b->unit != UNIF_BALANCE_BLOCKS) return UNIF_EINVAL;
     return UNIF_OK;
 }
@@ -378,24 +381,24 @@ BalanceShape balance_shape(const unif_moe_config* c, const unif_moe_balance* b, 
     BalanceShape s;
     const int N = std::max(c->n_tokens, 1);
     s.group = b->tokens_per_group > 0 ? b->tokens_per_group : N;
-    s.groups = b->tokens_per_group > 0 ? ceil_div(c->n_tokens, s.group) : 1;
+    s.groups = b->tokens_per_group > 0 ? div_up(c->n_tokens, s.group) : 1;
     const int longest = std::min(s.group, N);
     s.piece = longest <= kBalOnePiece ? longest : kBalPiece;
-    s.pieces = ceil_div(longest, s.piece);
-    s.waves = std::min(kBalWaves, ceil_div(s.piece, 64));
+    s.pieces = div_up(longest, s.piece);
+    s.waves = std::min(kBalWaves, div_up(s.piece, 64));
     // waves of 16 lanes' columns, an even number per workgroup
     const int most = balance_waves(c->n_experts);
-    const int waves = ceil_div(c->d_model, 16 * kBalNC);
-    s.slabs = ceil_div(waves, most);
-    s.cols = ceil_div(ceil_div(waves, s.slabs), 2) * 2;
+    const int waves = div_up(c->d_model, 16 * kBalNC);
+    s.slabs = div_up(waves, most);
+    s.cols = div_up(div_up(waves, s.slabs), 2) * 2;
     // Token ranges of whole 16-token steps, for the workgroups that run at once: more, of which some run in a second
     // round, cost more than the last ones' idle units, and their partial sums more
     // traffic. 131,072 x 1,024, K = 32 (two slabs): 64 ranges 545 us, 128 328, 170
     // 460, 256 372, 512 387; 50,432 x 768, K = 16: 64 184, 128 125, 170 156, 256
     // 129, 512 138; 4,096 x 768, K = 8: 64 27, 128 23, 256 27.
-    const int steps = ceil_div(N, 16), ranges = std::max(1, cus * (most / s.cols) / s.slabs);
-    s.steps = ceil_div(steps, ranges);
-    s.parts = ceil_div(steps, s.steps);
+    const int steps = div_up(N, 16), ranges = std::max(1, cus * (most / s.cols) / s.slabs);
+    s.steps = div_up(steps, ranges);
+    s.parts = div_up(steps, s.steps);
     return s;
 }
 
@@ -423,7 +426,7 @@ void launch_balance_grad(const BalanceShape& s, const BalanceParams& p, unsigned
 }
 template <class T>
 void launch_balance_grad(const BalanceShape& s, const BalanceParams& p, unsigned extra, hipStream_t st) {
-    switch (ceil_div(p.K, 16)) {
+    switch (div_up(p.K, 16)) {
         case 1: return launch_balance_grad<T, 1>(s, p, extra, st);
         case 2: return launch_balance_grad<T, 2>(s, p, extra, st);
         case 3: return launch_balance_grad<T, 3>(s, p, extra, st);

@@ -449,3 +449,22 @@ def test_offsets_past_32_bits():
         del y, h
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     torch.cuda.empty_cache()
+
+
+def test_absent_stream_in_mixed_types():
+    """No x and no y beside an fp32 stream, a workspace at an odd address, and
+    both gradients from one tensor."""
+    print("\n[gpu] residual: absent stream", flush=True)
+    for d in (4, 7, 129, 2049):
+        c = Case(1, d, ("bf16", "f32", "f32"), gate=True)
+        _, want = c.forward(x=torch.zeros_like(c.x))
+        _, h = c.forward(x=None, y=None)
+        assert torch.equal(h, want)
+        c = Case(40, d, ("f32", "f32", "f32"), gate=True, per=7)
+        c.dh = c.dy
+        size = ops.residual_backward_workspace_size(c.res)
+        first, ws = c.backward(), torch.empty(size + 3, dtype=torch.uint8, device=DEV)
+        o = c.backward(ws=ws[3:])
+        assert all(torch.equal(o[k], first[k]) for k in o)
+        for k, v in o.items():
+            check(k, v, *c.backward64()[k])
