@@ -88,6 +88,8 @@ __device__ __forceinline__ void balance_finish_group(const BalanceParams& p, int
 // expert order in LDS (selected experts with the sign bit set), then lane j +
 // w h adds expert j's entries of the h-th of 64 / w runs of tokens, w the
 // experts rounded up to a power of two. A group of one piece is finished here.
+// Latency bound: all of a tile's loads are issued at once (50,432 tokens, K = 16: 8.8
+// us, 0.8 TB/s; entry by entry and token by token it took 46).
 constexpr int kBalWaves = 8, kBalBatch = 16;
 __host__ __device__ __forceinline__ int balance_wave_words(int K) { return 64 * (K | 1) + 2 * 64; }
 
@@ -283,7 +285,10 @@ __global__ __launch_bounds__(1024) void balance_mean_kernel(BalanceParams p) { b
 // number, so a tile is whole steps), eight lanes per token: a wave loads its
 // tokens' entries when the tile before begins, the slopes of their experts after
 // its first step, and writes dl behind its last; one barrier per tile. Padded
-// tokens have dl = 0, and their rows of X are not used.
+// tokens have dl = 0, and their rows of X are not used. HBM bound: 50,432 x 768 bf16,
+// K = 16 86 us, 4.7 TB/s of 10 bytes an element; 131,072 x 1,024, K = 32 285 us, 4.9
+// TB/s, the matrix cores busy 40% of it at 153 TFLOP/s. In 8 columns a lane, fewer
+// waves fit: 408 us for 372 there, before the ranges were sized to run at once.
 template <class T, int NC>
 struct BalRow {
     typedef T mem __attribute__((ext_vector_type(NC), aligned(sizeof(T))));

@@ -83,7 +83,7 @@ struct RowShape {
     int lpr, chunks, threads, rows, blocks;
     int teams() const { return lpr == 0 ? blocks : blocks * (threads / lpr); }
 };
-// Rows of up to 1,024 columns are a part of a wave's, 2 or 3 chunks of E columns
+// Rows of up to 1,024 columns are a part of a wave's, 2 or 3 chunks of kCols columns
 // per lane (a whole wave's also 4), the fewest columns that cover the row, more
 // lanes rather than more chunks: 2 chunks against 4 on half the lanes, 200,000 x
 // 128 bf16 42 us and 49, 400,000 x 64 45 and 59, 60,000 x 512 50 and 53; 3 chunks
@@ -92,15 +92,15 @@ struct RowShape {
 RowShape narrow_shape(int d, int threads) {
     RowShape s{};
     s.lpr = 8;
-    while (s.lpr < kWave && s.lpr * 3 * E < d) s.lpr *= 2;
-    s.chunks = s.lpr * 2 * E >= d ? 2 : s.lpr * 3 * E >= d ? 3 : 4;
+    while (s.lpr < kWave && s.lpr * 3 * kCols < d) s.lpr *= 2;
+    s.chunks = s.lpr * 2 * kCols >= d ? 2 : s.lpr * 3 * kCols >= d ? 3 : 4;
     s.threads = threads;
     return s;
 }
 RowShape wide_shape(int d) {
     RowShape s{};
     s.chunks = 2;
-    s.threads = div_up(d, kWave * 2 * E) * kWave;
+    s.threads = div_up(d, kWave * 2 * kCols) * kWave;
     return s;
 }
 // The tokens dealt to at most `waves` waves per compute unit.
@@ -133,7 +133,7 @@ void with_shape(const RowShape& s, F f) {
     return s.lpr == 8 ? f(two, l8) : s.lpr == 16 ? f(two, l16) : s.lpr == 32 ? f(two, l32) : f(two, l64);
 }
 
-constexpr int kNarrowD = kWave * 4 * E;
+constexpr int kNarrowD = kWave * 4 * kCols;
 // Forward: many more waves than run at once, so that the last ones of a launch
 // leave little of the chip idle: 65,536 x 1,024 bf16 113.5 us with 16 waves per
 // compute unit, 111 with 32, 108.8 with 64; 200,000 x 128 46.6, 44.9 and 42.5.
