@@ -262,7 +262,16 @@ __device__ __forceinline__ void balance_mean(const BalanceParams& p) {
     __shared__ double part[16];
     const int nw = (int)blockDim.x >> 6, w = (int)threadIdx.x >> 6;
     double s = 0.0;
-    for (int64_t g = threadIdx.x; g < p.groups; g += blockDim.x) s += p.gloss[g];
+    for (int64_t g0 = threadIdx.x; g0 < p.groups; g0 += 8 * (int64_t)blockDim.x) {
+        double v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t g = g0 + i * (int64_t)blockDim.x;
+            v[i] = p.gloss[g < p.groups ? g : g0];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += g0 + i * (int64_t)blockDim.x < p.groups ? v[i] : 0.0;
+    }
     s = wave_sum(s);
     if (lane_id() == 0) part[w] = s;
     __syncthreads();
