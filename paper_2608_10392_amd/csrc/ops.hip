@@ -76,7 +76,8 @@ size_t gate_bytes(const unif_moe_residual* r) { return (size_t)gate_rows(r) * r-
 bool gate_grouped(const unif_moe_residual* r) { return r->gate != nullptr && gate_rows(r) > 1; }
 
 // LDS that the kernels declare beside what their launch asks for.
-constexpr size_t kTeamLds = 2 * kWideWaves * 4 * sizeof(float), kCountLds = kBalWaves * (kWave * 12 + 8);
+constexpr size_t kTeamLds = 2 * kWideWaves * 4 * sizeof(float), kCountLds = kBalWaves * (kWave * 12 + 8) + 4 * kWave,
+                 kSlopeLds = 8 * (kWave * kBalWaves + 2 * kWave + 2) + 4 * kWave;
 
 // Lanes per row (0: the workgroup) and the launch that covers the tokens.
 struct RowShape {
@@ -368,10 +369,11 @@ int32_t check_balance(const unif_moe_config* c, const unif_moe_balance* b) {
     return UNIF_OK;
 }
 
-// Groups of up to this many tokens are one workgroup's in the count, which then
-// finishes them; longer ones are counted in pieces of kBalPiece.
 constexpr int kBalNC = 4;   // columns per lane
-constexpr int kBalOnePiece = 1024, kBalPiece = 512;
+// Groups of up to kBalOnePiece tokens are one workgroup's in the count, which then
+// finishes them; longer ones are counted in pieces of at least kBalPiece tokens, at
+// most kBalPieces, since every piece's workgroup adds them all before its dl.
+constexpr int kBalOnePiece = 1024, kBalPiece = 512, kBalPieces = 256;
 
 struct BalanceShape {
     int group, groups, pieces, piece, waves;   // count
@@ -383,27 +385,27 @@ BalanceShape balance_shape(const unif_moe_config* c, const unif_moe_balance* b, 
     s.group = b->tokens_per_group > 0 ? b->tokens_per_group : N;
     s.groups = b->tokens_per_group > 0 ? div_up(c->n_tokens, s.group) : 1;
     const int longest = std::min(s.group, N);
-    s.piece = longest <= kBalOnePiece ? longest : kBalPiece;
+    s.piece = longest <= kBalOnePiece ? longest : std::max(kBalPiece, div_up(div_up(longest, kBalPieces), 64) * 64);
     s.pieces = div_up(longest, s.piece);
     s.waves = std::min(kBalWaves, div_up(s.piece, 64));
-    // waves of 16 lanes' columns, an even number per workgroup
-    const int most = balance_waves(c->n_experts);
-    const int waves = div_up(c->d_model, 16 * kBalNC);
-    s.slabs = div_up(waves, most);
-    s.cols = div_up(div_up(waves, s.slabs), 2) * 2;
-    // Token ranges of whole 16-token steps, for the workgroups that run at once: more, of which some run in a second
-    // round, cost more than the last ones' idle units, and their partial sums more
-    // traffic. 131,072 x 1,024, K = 32 (two slabs): 64 ranges 545 us, 128 328, 170
-    // 460, 256 372, 512 387; 50,432 x 768, K = 16: 64 184, 128 125, 170 156, 256
-    // 129, 512 138; 4,096 x 768, K = 8: 64 27, 128 23, 256 27.
-    const int steps = div_up(N, 16), ranges = std::max(1, cus * (most / s.cols) / s.slabs);
+    // strips of 16 lanes' columns, a wave each, at most four per workgroup (one per
+    // SIMD; with up to eight, 50,000 x 1,152, K = 20 153 -> 161 us, K = 36 92 -> 97)
+    const int strips = div_up(c->d_model, 16 * kBalNC);
+    s.slabs = div_up(strips, kBalStrips);
+    s.cols = div_up(strips, s.slabs);
+    // Token ranges of whole 16-token steps, for the waves that run at once: more, of
+    // which some run in a second round, cost more than the last ones' idle units, and
+    // their partial sums more traffic. In an earlier form, 131,072 x 1,024, K = 32: 64
+    // ranges 545 us, 128 (all at once) 328, 170 460, 256 372, 512 387; 50,432 x 768, K
+    // = 16: 64 184, 128 125, 170 156, 256 129, 512 138.
+    const int steps = div_up(N, 16), ranges = std::max(1, cus * (balance_waves(c->n_experts) / s.cols) / s.slabs);
     s.steps = div_up(steps, ranges);
     s.parts = div_up(steps, s.steps);
     return s;
 }
 
 struct BalancePlan {
-    size_t sums, slope, gloss, part, total;
+    size_t sums, gloss, dl, part, total;
 };
 BalancePlan plan_balance(const unif_moe_config* c, const unif_moe_balance* b) {
     const BalanceShape s = balance_shape(c, b, kMaxCus);
@@ -411,8 +413,8 @@ BalancePlan plan_balance(const unif_moe_config* c, const unif_moe_balance* b) {
     Carver cv;
     BalancePlan p;
     p.sums = cv.take(8 * units * (2 * K + 2));
-    p.slope = cv.take(4 * s.groups * K);
     p.gloss = cv.take(8 * (size_t)s.groups);
+    p.dl = cv.take(4 * (size_t)c->n_tokens * (div_up(c->n_experts, 16) * 16));
     p.part = cv.take(4 * (size_t)s.parts * K * c->d_model);
     p.total = cv.cur + 256;
     return p;
@@ -421,8 +423,13 @@ BalancePlan plan_balance(const unif_moe_config* c, const unif_moe_balance* b) {
 template <class T, int KT>
 void launch_balance_grad(const BalanceShape& s, const BalanceParams& p, unsigned extra, hipStream_t st) {
     const dim3 grid((unsigned)s.parts + extra, (unsigned)s.slabs);
-    const size_t tile = 8 * (size_t)s.cols, lds = 2 * tile * (16 * KT + 4 + 1) * sizeof(float);
-    balance_grad_kernel<T, KT, kBalNC><<<grid, (unsigned)s.cols * kWave, lds, st>>>(p);
+    const unsigned threads = (unsigned)s.cols * kWave;
+    if (p.dX != nullptr && p.dW != nullptr && p.dX_in != nullptr)
+        balance_grad_kernel<T, KT, kBalNC, 1><<<grid, threads, 0, st>>>(p);
+    else if (p.dX != nullptr && p.dW != nullptr)
+        balance_grad_kernel<T, KT, kBalNC, 2><<<grid, threads, 0, st>>>(p);
+    else
+        balance_grad_kernel<T, KT, kBalNC, 0><<<grid, threads, 0, st>>>(p);
 }
 template <class T>
 void launch_balance_grad(const BalanceShape& s, const BalanceParams& p, unsigned extra, hipStream_t st) {
@@ -504,10 +511,12 @@ int32_t unif_moe_balance_loss(const unif_moe_config* cfg, const unif_moe_balance
     p.loss = loss;
     p.counts = counts;
     p.sums = reinterpret_cast<uint64_t*>(ws + plan.sums);
-    p.slope = reinterpret_cast<float*>(ws + plan.slope);
     p.gloss = reinterpret_cast<double*>(ws + plan.gloss);
     p.part = reinterpret_cast<float*>(ws + plan.part);
     p.parts = N > 0 ? sh.parts : 0;
+    p.KP = div_up(K, 16) * 16;
+    const bool grads = N > 0 && (dX != nullptr || dW_router != nullptr);
+    p.dl = grads ? reinterpret_cast<float*>(ws + plan.dl) : nullptr;
     p.steps = sh.steps;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (sh.groups > 0) {
@@ -517,13 +526,16 @@ int32_t unif_moe_balance_loss(const unif_moe_config* cfg, const unif_moe_balance
         balance_count_kernel<<<flat_grid((size_t)sh.groups * sh.pieces), (unsigned)sh.waves * kWave, lds, st>>>(p);
         UNIF_LAUNCH_CHECK();
         if (sh.pieces > 1) {
-            balance_group_kernel<<<flat_grid((size_t)sh.groups), kBalGroupThreads, 0, st>>>(p);
+            const size_t all = kBalWaves * sizeof(float) * (size_t)balance_wave_words(K);
+            const int32_t fits = allow_lds(balance_slope_kernel, (grads ? all : 0) + kSlopeLds);
+            if (fits != UNIF_OK) return fits;
+            balance_slope_kernel<<<flat_grid((size_t)sh.groups * (grads ? sh.pieces : 1)), kWave * kBalWaves, grads ? all : 0, st>>>(p);
             UNIF_LAUNCH_CHECK();
         }
     }
     // The groups' mean: with one group it is written already, else beside the
     // gradients where those are wanted.
-    const bool grads = N > 0 && (dX != nullptr || dW_router != nullptr), mean = sh.groups != 1;
+    const bool mean = sh.groups != 1;
     if (mean && !grads) {
         balance_mean_kernel<<<1, 1024, 0, st>>>(p);
         UNIF_LAUNCH_CHECK();
