@@ -138,10 +138,12 @@ constexpr int kNarrowD = kWave * 4 * kCols;
 // Forward: many more waves than run at once, so that the last ones of a launch
 // leave little of the chip idle: 65,536 x 1,024 bf16 113.5 us with 16 waves per
 // compute unit, 111 with 32, 108.8 with 64; 200,000 x 128 46.6, 44.9 and 42.5.
-// Fewer for wide rows, whose teams are few and share barriers: 8,192 x 8,192 113,
-// 116.5 and 117.5, 16,384 x 2,048 67, 63 and 66.
+// Wide rows' teams are few and come in whole workgroups: about as many waves as run
+// at once. 16, 32 and 64 waves: 540 x 6,656 11.8, 15.8 and 16.5 us; 1,068 x 4,400
+// 15.7, 22.2 and 25.8; 16,384 x 5,120 149, 158 and 164; but 4,099 x 5,120 47, 45 and
+// 47, 16,384 x 2,048 63, 62 and 64.
 RowShape forward_shape(const unif_moe_residual* r, int cus) {
-    if (r->d_model > kNarrowD) return cover(wide_shape(r->d_model), r->n_tokens, cus, 32);
+    if (r->d_model > kNarrowD) return cover(wide_shape(r->d_model), r->n_tokens, cus, 16);
     return cover(narrow_shape(r->d_model, 256), r->n_tokens, cus, 64);
 }
 // Backward: as many waves as run at once (two per SIMD, by their registers), so
