@@ -1,5 +1,8 @@
 """Device-resident UniF-MoE layer: moves one layer's inputs to the GPU once
 and calls the HIP library on them (torch supplies memory and streams)."""
+import contextlib
+import functools
+
 import numpy as np
 
 from . import _lib, ops
@@ -18,6 +21,20 @@ def to_device(a, dtype_name, device):
     else:
         t = torch.from_numpy(np.ascontiguousarray(a))
     return t.to(device)
+
+
+def _on_stream(method):
+    """Runs ``method`` with its ``stream`` argument (a torch stream, a raw handle
+    or None) current: what it allocates belongs to that stream, so memory it
+    frees on return is not handed out before the stream's work on it is done."""
+    @functools.wraps(method)
+    def run(self, *args, stream=None, **kwargs):
+        import torch
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device=getattr(self, "layer", self).device)
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            return method(self, *args, stream=stream, **kwargs)
+    return run
 
 
 class DeviceLayer:
@@ -89,7 +106,8 @@ class DeviceLayer:
                             stream=stream)
         return g
 
-    def diversity_loss(self, weight, dW_router, stream=None):
+    @_on_stream
+    def diversity_loss(self, weight, dW_router, *, stream=None):
         """L_div of the router as a device scalar; weight times its gradient is
         added to ``dW_router``."""
         import torch
@@ -98,7 +116,8 @@ class DeviceLayer:
         _lib.diversity_loss(self.cfg, self.W_router, weight, loss, dW_router, ws, stream=stream)
         return loss
 
-    def balance_loss(self, bal, dX=None, dW_router=None, stream=None):
+    @_on_stream
+    def balance_loss(self, bal, dX=None, dW_router=None, *, stream=None):
         """Balance loss and per-expert loads (device tensors) over the routing
         record of the last forward or route; weight times the loss's gradient is
         added to ``dX`` and ``dW_router`` where given."""
@@ -159,7 +178,8 @@ class DeviceBlock:
         self.behind = ops.make_residual(dict(size, **behind))
         self.stream = torch.bfloat16 if size["stream_dtype"] == "bf16" else torch.float32
 
-    def forward(self, x, stream=None):
+    @_on_stream
+    def forward(self, x, *, stream=None):
         import torch
         L = self.layer
         L.X = torch.empty((L.cfg["n_tokens"], L.cfg["d_model"]), dtype=L.Y.dtype, device=L.device)
@@ -169,7 +189,8 @@ class DeviceBlock:
         ops.residual_forward(self.behind, x, f, L.valid, y, None, stream=stream)
         return y
 
-    def backward(self, x, dy, balance=None, diversity=0.0, stream=None):
+    @_on_stream
+    def backward(self, x, dy, balance=None, diversity=0.0, *, stream=None):
         """Gradients of the last forward: dx, the layer's (dW_up, dW_down,
         dW_router) and the parameters', and the losses."""
         import torch

@@ -15,7 +15,7 @@ import pytest
 import torch
 
 import oracle.unif_moe_oracle as O
-from paper_2608_10392_amd import ops
+from paper_2608_10392_amd import _lib, ops
 from paper_2608_10392_amd.layer import DeviceBlock, DeviceLayer
 from synth import generate, get_config, layer_config
 from tests import parity
@@ -109,3 +109,64 @@ def test_training_step(dtype, stream):
         print(f"[gpu] {key}: {err:.1e} x max", flush=True)
         assert err <= tol, f"{key}: {err:.2e} of the largest value"
     assert bool((got["dx"][torch.from_numpy(valid == 0).to(DEV)] == 0).all())
+
+
+def step_inputs():
+    """A small fp32 block, its input and an output gradient."""
+    g = generate(get_config("tiny_f32", n_tokens=320, d_model=128, n_experts=5, n_blocks=4, block_width=64, max_shared=4))
+    rng = np.random.default_rng(4)
+    rand = lambda *s: torch.from_numpy(rng.standard_normal(s).astype(np.float32)).to(DEV)
+    dev = DeviceLayer(layer_config(g["cfg"]), g["X"], None, g["W_router"], g["prototypes"], g["W_up"], g["W_down"],
+                      device=DEV)
+    block = DeviceBlock(dev, dict(in_norm="rms", out_norm="layer", in_eps=EPS, out_eps=EPS, in_gamma=1 + 0.1 * rand(128),
+                                  out_gamma=1 + 0.1 * rand(128), out_beta=0.1 * rand(128)))
+    return block, rand(320, 128), rand(320, 128)
+
+
+def step(block, x, dy, stream=None):
+    y = block.forward(x, stream=stream)
+    return dict(block.backward(x, dy, dict(tokens_per_group=64, weight=0.5), 0.25, stream=stream), y=y)
+
+
+def agree(got, want):
+    # the layer's own sums may come in another order: a few fp32 steps of the largest value
+    for key, w in want.items():
+        err = float((got[key].double() - w.double()).abs().max())
+        assert err <= 1e-5 * float(w.double().abs().max()), f"{key}: {err:.2e}"
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_step_on_another_stream(raw, monkeypatch):
+    """What a step allocates on another stream belongs to that stream."""
+    print(f"\n[gpu] block step on another stream, raw handle {raw}", flush=True)
+    block, x, dy = step_inputs()
+    want = step(block, x, dy)
+    torch.cuda.synchronize()
+    side, seen = torch.cuda.Stream(), []
+    alloc = _lib.alloc_workspace
+    monkeypatch.setattr(_lib, "alloc_workspace",
+                        lambda *a: (seen.append(torch.cuda.current_stream().cuda_stream), alloc(*a))[1])
+    got = step(block, x, dy, side.cuda_stream if raw else side)
+    side.synchronize()
+    assert seen and set(seen) == {side.cuda_stream}
+    assert torch.cuda.current_stream().cuda_stream != side.cuda_stream
+    agree(got, want)
+
+
+def test_step_captured():
+    """A captured step's replays, with eager steps between them."""
+    print("\n[gpu] block step captured", flush=True)
+    block, x, dy = step_inputs()
+    want = {k: v.clone() for k, v in step(block, x, dy).items()}
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(block, x, dy)
+    for _ in range(3):
+        for v in got.values():
+            v.fill_(-1)
+        graph.replay()
+        torch.cuda.synchronize()
+        agree(got, want)
+        agree(step(block, x, dy), want)
+        torch.cuda.synchronize()
