@@ -2,25 +2,35 @@
 and calls the HIP library on them (torch supplies memory and streams)."""
 import contextlib
 import functools
+import math
 
 import numpy as np
 
 from . import _lib, ops
 
 
-def to_device(a, dtype_name, device):
-    """numpy array -> torch device tensor; bf16 data arrives as uint16 bits.
-    Tensors are moved as they are."""
+def to_device(a, dtype_name, device, name="array", shape=None):
+    """numpy array or torch tensor -> contiguous torch device tensor of the
+    format: bf16 data arrives as 16-bit words (or as a bfloat16 tensor), f32
+    data as float32. Other types are refused, and with ``shape`` what does not
+    hold it: other sizes, unless only the first dimension is larger."""
     import torch
     if a is None:
         return None
-    if torch.is_tensor(a):
-        return a.to(device)
-    if dtype_name == "bf16":
-        t = torch.from_numpy(np.ascontiguousarray(a).view(np.int16)).view(torch.bfloat16)
-    else:
-        t = torch.from_numpy(np.ascontiguousarray(a))
-    return t.to(device)
+    if not torch.is_tensor(a):
+        a = np.ascontiguousarray(a)
+        if dtype_name == "bf16" and (a.dtype.kind not in "fc" or a.dtype.name == "bfloat16"):
+            a = a.view(np.int16)   # the words, however they are typed
+        a = torch.from_numpy(a)
+    if dtype_name == "bf16" and a.dtype in (torch.int16, torch.uint16):
+        a = a.view(torch.bfloat16)
+    want = torch.bfloat16 if dtype_name == "bf16" else torch.float32
+    if a.dtype != want:
+        ops._refuse("to_device", f"{name} is {a.dtype}, not {want}")
+    if shape is not None and a.numel() != math.prod(shape):
+        if a.dim() != len(shape) or a.shape[1:] != shape[1:] or a.shape[0] < shape[0]:
+            ops._refuse("to_device", f"{name} is {tuple(a.shape)}, not {tuple(shape)}")
+    return a.to(device).contiguous()
 
 
 def _on_stream(method):
@@ -41,8 +51,9 @@ class DeviceLayer:
     """Inputs of one layer on the device, plus output, record and workspace.
 
     ``cfg`` is a layer description dict (dtype "bf16" or "f32"); arrays are
-    numpy: X and the expert weights as bf16 bits (uint16) or float32, the
-    router and prototypes as float32, ``valid`` as uint8 or None.
+    numpy: X and the expert weights as bf16 bits (uint16) or float32 (or
+    tensors, see to_device), the router and prototypes as float32, ``valid`` as
+    uint8 or None.
     """
 
     def __init__(self, cfg, X, valid, W_router, prototypes, W_up=None, W_down=None,
@@ -52,12 +63,13 @@ class DeviceLayer:
         self.device = device
         dt = cfg["dtype"]
         N, d, K = cfg["n_tokens"], cfg["d_model"], cfg["n_experts"]
-        self.X = to_device(X, dt, device)
+        H = cfg["n_blocks"] * cfg["block_width"]
+        self.X = to_device(X, dt, device, "X", (N, d))
         self.valid = None if valid is None else torch.from_numpy(np.ascontiguousarray(valid, np.uint8)).to(device)
         self.W_router = to_device(np.asarray(W_router, np.float32), "f32", device)
         self.prototypes = to_device(np.asarray(prototypes, np.float32), "f32", device)
-        self.W_up = to_device(W_up, dt, device)
-        self.W_down = to_device(W_down, dt, device)
+        self.W_up = to_device(W_up, dt, device, "W_up", (K + 1, H, d))
+        self.W_down = to_device(W_down, dt, device, "W_down", (K + 1, d, H))
         self.Y = torch.empty((N, d), dtype=torch.bfloat16 if dt == "bf16" else torch.float32,
                              device=device)
         self.routing = _lib.alloc_routing(N, K, device)
@@ -77,8 +89,8 @@ class DeviceLayer:
         """The transformer block around the layer (``blk`` as
         synth.block_inputs returns it: numpy parameters, moved to the device
         on each call). ``X`` replaces the layer input (the residual stream)."""
-        dt = self.cfg["dtype"]
-        Xd = self.X if X is None else to_device(X, dt, self.device)
+        c = self.cfg
+        Xd = self.X if X is None else to_device(X, c["dtype"], self.device, "X", (c["n_tokens"], c["d_model"]))
         b = dict(norm=blk["norm"], residual=blk["residual"], ln_eps=blk["ln_eps"])
         for k in ("ln_gamma", "ln_beta", "b_up", "b_down"):
             b[k] = None if blk.get(k) is None else to_device(np.asarray(blk[k], np.float32), "f32",
@@ -90,16 +102,16 @@ class DeviceLayer:
         return self.Y
 
     def backward(self, dY, stream=None):
-        """Gradients of sum(dY * Y) (numpy dY in the layer's format): dict of
+        """Gradients of sum(dY * Y) (dY in the layer's format, see to_device): dict of
         fp32 device tensors dX, dW_up, dW_down, dW_router."""
         import torch
         c = self.cfg
         N, d, K = c["n_tokens"], c["d_model"], c["n_experts"]
         H = c["n_blocks"] * c["block_width"]
+        dYd = to_device(dY, c["dtype"], self.device, "dY", (N, d))
         f = dict(dtype=torch.float32, device=self.device)
         g = dict(dX=torch.empty((N, d), **f), dW_up=torch.empty((K + 1, H, d), **f),
                  dW_down=torch.empty((K + 1, d, H), **f), dW_router=torch.empty((K + 1, d), **f))
-        dYd = to_device(dY, c["dtype"], self.device)
         ws = _lib.alloc_workspace(_lib.layer_backward_workspace_size(c), self.device)
         _lib.layer_backward(c, self.X, self.valid, self.W_router, self.prototypes, self.W_up,
                             self.W_down, dYd, g["dX"], g["dW_up"], g["dW_down"], g["dW_router"], ws,
