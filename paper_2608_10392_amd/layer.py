@@ -41,7 +41,9 @@ def _on_stream(method):
     def run(self, *args, stream=None, **kwargs):
         import torch
         if isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(stream, device=getattr(self, "layer", self).device)
+            # 0 is the null stream's handle, which ExternalStream takes for none at all
+            device = getattr(self, "layer", self).device
+            stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
         with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
             return method(self, *args, stream=stream, **kwargs)
     return run

@@ -1,0 +1,80 @@
+"""Which stream and device the calls of DeviceLayer and DeviceBlock run on: a
+stand-in for torch's streams records them (no GPU needed)."""
+import contextlib
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_10392_amd import _lib, ops
+from paper_2608_10392_amd.layer import DeviceBlock, DeviceLayer
+
+N, D, K, B, M = 4, 8, 2, 2, 4
+CFG = dict(n_tokens=N, d_model=D, n_experts=K, n_blocks=B, block_width=M, mass_threshold=0.7, dtype="f32")
+
+
+class Stream:
+    def __init__(self, handle):
+        self.cuda_stream = handle
+
+
+class Streams:
+    """Streams by handle; 0 is the default stream. `seen` holds, for every
+    workspace and every call of the library, the stream current then and (for
+    calls) the handle it was given."""
+
+    def __init__(self, monkeypatch):
+        self.now, self.seen = Stream(0), []
+        cuda = torch.cuda
+        monkeypatch.setattr(cuda, "default_stream", lambda device=None: Stream(0))
+        monkeypatch.setattr(cuda, "current_stream", lambda device=None: self.now)
+        # as torch's: a handle of 0 counts as not given, a stream of torch's own comes back
+        monkeypatch.setattr(cuda, "ExternalStream", lambda handle, device=None: Stream(handle or 0xABCD))
+        monkeypatch.setattr(cuda, "stream", self.use)
+        alloc = _lib.alloc_workspace
+        monkeypatch.setattr(_lib, "alloc_workspace", lambda *a: (self.note("workspace"), alloc(*a))[1])
+        for mod in (_lib, ops):
+            for name in ("route", "layer_forward", "block_forward", "layer_backward", "stats", "diversity_loss",
+                         "balance_loss", "residual_forward", "residual_backward"):
+                if hasattr(mod, name):
+                    monkeypatch.setattr(mod, name, lambda *a, name=name, stream=None, **k: self.note(name, stream))
+                    monkeypatch.setattr(mod, name + "_workspace_size", lambda *a: 16, raising=False)
+
+    def note(self, what, stream=None):
+        handle = self.now.cuda_stream if stream is None else getattr(stream, "cuda_stream", stream)
+        self.seen.append((what, self.now.cuda_stream, handle))
+
+    @contextlib.contextmanager
+    def use(self, stream):
+        was, self.now = self.now, stream
+        yield
+        self.now = was
+
+
+def make():
+    z = lambda *s: np.zeros(s, np.float32)
+    dev = DeviceLayer(CFG, z(N, D), None, z(K + 1, D), z(B, D), z(K + 1, B * M, D), z(K + 1, D, B * M), device="cpu")
+    block = DeviceBlock.__new__(DeviceBlock)
+    block.layer, block.params, block.before, block.behind = dev, {}, None, None
+    return dev, block
+
+
+X = torch.zeros(N, D)
+BLK = dict(norm="none", residual=True, ln_eps=1e-6)
+NEW = dict(block_forward=lambda dev, block, **s: block.forward(X, **s),
+           block_backward=lambda dev, block, **s: block.backward(X, X, {}, 0.5, **s),
+           balance=lambda dev, block, **s: dev.balance_loss({}, **s),
+           diversity=lambda dev, block, **s: dev.diversity_loss(0.5, X, **s))
+
+
+@pytest.mark.parametrize("name", list(NEW))
+def test_handles(name, monkeypatch):
+    """A raw handle, 0 (the null stream) among them, is the stream that is used
+    and that the call's memory belongs to."""
+    streams, (dev, block) = Streams(monkeypatch), make()
+    for handle in (0, 77):
+        for now in (Stream(0), Stream(5)):
+            streams.now, streams.seen = now, []
+            NEW[name](dev, block, stream=handle)
+            assert streams.seen and {s[1:] for s in streams.seen} == {(handle, handle)}, streams.seen
+            assert streams.now is now
