@@ -2,6 +2,7 @@
 and calls the HIP library on them (torch supplies memory and streams)."""
 import contextlib
 import functools
+import inspect
 import math
 
 import numpy as np
@@ -37,15 +38,25 @@ def _on_stream(method):
     """Runs ``method`` with its ``stream`` argument (a torch stream, a raw handle
     or None) current: what it allocates belongs to that stream, so memory it
     frees on return is not handed out before the stream's work on it is done."""
+    args_of = inspect.signature(method).parameters
+    at = list(args_of).index("stream") - 1   # among the arguments behind self
+    by_position = args_of["stream"].kind is inspect.Parameter.POSITIONAL_OR_KEYWORD
+
     @functools.wraps(method)
-    def run(self, *args, stream=None, **kwargs):
+    def run(self, *args, **kwargs):
         import torch
+        given = by_position and len(args) > at
+        stream = args[at] if given else kwargs.get("stream")
         if isinstance(stream, int):
             # 0 is the null stream's handle, which ExternalStream takes for none at all
             device = getattr(self, "layer", self).device
             stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+        if given:
+            args = (*args[:at], stream, *args[at + 1:])
+        else:
+            kwargs["stream"] = stream
         with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-            return method(self, *args, stream=stream, **kwargs)
+            return method(self, *args, **kwargs)
     return run
 
 
@@ -55,7 +66,9 @@ class DeviceLayer:
     ``cfg`` is a layer description dict (dtype "bf16" or "f32"); arrays are
     numpy: X and the expert weights as bf16 bits (uint16) or float32 (or
     tensors, see to_device), the router and prototypes as float32, ``valid`` as
-    uint8 or None.
+    uint8 or None. The calls share the output, the record and the workspaces:
+    those on different streams, and replays of graphs that hold such calls, are
+    ordered by the caller, who keeps the layer until their work is done.
     """
 
     def __init__(self, cfg, X, valid, W_router, prototypes, W_up=None, W_down=None,
@@ -79,6 +92,7 @@ class DeviceLayer:
         self.ws_route = None
         self.ws_stats = None
 
+    @_on_stream
     def forward(self, stream=None, routing=True):
         if self.ws_forward is None:
             self.ws_forward = _lib.alloc_workspace(_lib.layer_forward_workspace_size(self.cfg), self.device)
@@ -87,6 +101,7 @@ class DeviceLayer:
                            routing=self.routing if routing else None, stream=stream)
         return self.Y
 
+    @_on_stream
     def block_forward(self, blk, X=None, stream=None, routing=True):
         """The transformer block around the layer (``blk`` as
         synth.block_inputs returns it: numpy parameters, moved to the device
@@ -103,6 +118,7 @@ class DeviceLayer:
                            routing=self.routing if routing else None, stream=stream)
         return self.Y
 
+    @_on_stream
     def backward(self, dY, stream=None):
         """Gradients of sum(dY * Y) (dY in the layer's format, see to_device): dict of
         fp32 device tensors dX, dW_up, dW_down, dW_router."""
@@ -145,6 +161,7 @@ class DeviceLayer:
                          dW_router, ws, stream=stream)
         return loss, counts
 
+    @_on_stream
     def route(self, out=None, stream=None):
         if self.ws_route is None:
             self.ws_route = _lib.alloc_workspace(_lib.route_workspace_size(self.cfg), self.device)
@@ -153,6 +170,7 @@ class DeviceLayer:
                    self.ws_route, stream=stream)
         return out
 
+    @_on_stream
     def stats(self, stream=None):
         if self.ws_stats is None:
             self.ws_stats = _lib.alloc_workspace(_lib.stats_workspace_size(self.cfg), self.device)

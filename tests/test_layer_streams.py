@@ -78,3 +78,37 @@ def test_handles(name, monkeypatch):
             NEW[name](dev, block, stream=handle)
             assert streams.seen and {s[1:] for s in streams.seen} == {(handle, handle)}, streams.seen
             assert streams.now is now
+
+
+OLD = dict(forward=lambda dev, *s, **k: dev.forward(*s, **k), route=lambda dev, *s, **k: dev.route(None, *s, **k),
+           stats=lambda dev, *s, **k: dev.stats(*s, **k), backward=lambda dev, *s, **k: dev.backward(X, *s, **k),
+           layer_block=lambda dev, *s, **k: dev.block_forward(BLK, None, *s, **k))
+
+
+@pytest.mark.parametrize("name", list(OLD))
+def test_layer_memory_belongs_to_the_stream(name, monkeypatch):
+    """Workspaces and outputs of a call on another stream are allocated on that
+    stream, whichever way it is given; without one, on the current stream."""
+    streams = Streams(monkeypatch)
+    for given, want in (((), 5), ((Stream(9),), 9), ((9,), 9), ((0,), 0)):
+        for by_name in (False, True):
+            dev, _ = make()
+            streams.now, streams.seen = Stream(5), []
+            OLD[name](dev, **dict(zip(("stream",), given))) if by_name else OLD[name](dev, *given)
+            assert [s[0] for s in streams.seen].count("workspace") == 1
+            assert {s[1:] for s in streams.seen} == {(want, want)}, streams.seen
+    with pytest.raises(TypeError):
+        OLD[name](dev, Stream(9), stream=Stream(9))
+
+
+def test_the_other_arguments_keep_their_places(monkeypatch):
+    streams, (dev, _) = Streams(monkeypatch), make()
+    seen = []
+    monkeypatch.setattr(_lib, "layer_forward", lambda *a, routing, stream: seen.append((routing is None, stream)))
+    s = Stream(3)
+    for call in (lambda: dev.forward(s, False), lambda: dev.forward(s, routing=False),
+                 lambda: dev.forward(stream=s, routing=False), lambda: dev.forward(routing=False, stream=s)):
+        assert call() is dev.Y and seen.pop() == (True, s)
+    assert dev.forward() is dev.Y and seen.pop() == (False, None)
+    out = object()
+    assert dev.route(out, s) is out and dev.route() is dev.routing
