@@ -36,8 +36,9 @@ def to_device(a, dtype_name, device, name="array", shape=None):
 
 def _on_stream(method):
     """Runs ``method`` with its ``stream`` argument (a torch stream, a raw handle
-    or None) current: what it allocates belongs to that stream, so memory it
-    frees on return is not handed out before the stream's work on it is done."""
+    or None: the layer's device's current one) current, and so its device: what
+    it allocates belongs to that stream, so memory it frees on return is not
+    handed out before the stream's work on it is done."""
     args_of = inspect.signature(method).parameters
     at = list(args_of).index("stream") - 1   # among the arguments behind self
     by_position = args_of["stream"].kind is inspect.Parameter.POSITIONAL_OR_KEYWORD
@@ -47,15 +48,21 @@ def _on_stream(method):
         import torch
         given = by_position and len(args) > at
         stream = args[at] if given else kwargs.get("stream")
+        device = getattr(self, "layer", self).Y.get_device()
         if isinstance(stream, int):
             # 0 is the null stream's handle, which ExternalStream takes for none at all
-            device = getattr(self, "layer", self).device
             stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
         if given:
             args = (*args[:at], stream, *args[at + 1:])
         else:
             kwargs["stream"] = stream
-        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+        if stream is not None:
+            current = torch.cuda.stream(stream)
+        elif device >= 0 and device != torch.cuda.current_device():
+            current = torch.cuda.device(device)
+        else:
+            current = contextlib.nullcontext()
+        with current:
             return method(self, *args, **kwargs)
     return run
 

@@ -112,3 +112,33 @@ def test_the_other_arguments_keep_their_places(monkeypatch):
     assert dev.forward() is dev.Y and seen.pop() == (False, None)
     out = object()
     assert dev.route(out, s) is out and dev.route() is dev.routing
+
+
+@pytest.mark.parametrize("name", list(NEW) + list(OLD))
+def test_the_device_of_the_layer_is_current(name, monkeypatch):
+    """A layer on another device than the current one: the call runs with its
+    device current, and afterwards the other one is again."""
+    Streams(monkeypatch)
+    now, seen = [0], []
+
+    @contextlib.contextmanager
+    def device(index):
+        was, now[0] = now[0], index
+        yield
+        now[0] = was
+
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: now[0])
+    dev, block = make()
+    monkeypatch.setattr(Streams, "note", lambda self, what, stream=None: seen.append(now[0]))
+
+    class OnTheSecond:
+        """The layer's output as it would be on device 1."""
+        def get_device(self):
+            return 1
+        dtype, shape, device = dev.Y.dtype, dev.Y.shape, dev.Y.device
+
+    monkeypatch.setattr(torch, "empty_like", lambda t, **k: torch.empty(t.shape, dtype=t.dtype))
+    dev.Y = OnTheSecond()
+    (NEW[name] if name in NEW else lambda d, b: OLD[name](d))(dev, block)
+    assert seen and set(seen) == {1} and now == [0]
