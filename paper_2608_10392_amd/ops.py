@@ -74,6 +74,14 @@ def _known(where, desc, keys):
         _refuse(where, f"unknown keys {sorted(set(desc) - keys)}")
 
 
+def _int32(where, desc, key, other=None):
+    """An integer of the description; ctypes would cut it to 32 bits."""
+    v = int(desc[key] if other is None else desc.get(key, other))
+    if not -1 << 31 <= v < 1 << 31:
+        _refuse(where, f"{key} {v} is past 32 bits")
+    return v
+
+
 class _Tensors:
     """Checks a call's tensors (all on one GPU) and yields their pointers."""
     __slots__ = ("where", "device")
@@ -141,8 +149,8 @@ def make_residual(desc):
     can share the structure."""
     import torch
     _known("make_residual", desc, RESIDUAL_KEYS)
-    n, d = int(desc["n_tokens"]), int(desc["d_model"])
-    per = int(desc.get("tokens_per_gate", 0))
+    n, d = (_int32("make_residual", desc, k) for k in ("n_tokens", "d_model"))
+    per = _int32("make_residual", desc, "tokens_per_gate", 0)
     r = Residual(n_tokens=n, d_model=d, dtype=_lib.DTYPES[desc["dtype"]],
                  stream_dtype=_lib.DTYPES[desc.get("stream_dtype", desc["dtype"])],
                  out_norm=ROW_NORMS[desc.get("out_norm", "none")], in_norm=ROW_NORMS[desc.get("in_norm", "none")],
@@ -204,7 +212,7 @@ def make_balance(bal):
     """Balance structure from a dict: tokens_per_group (0: one group), unit
     ("tokens", "blocks"), weight (1)."""
     _known("make_balance", bal, BALANCE_KEYS)
-    return Balance(tokens_per_group=int(bal.get("tokens_per_group", 0)),
+    return Balance(tokens_per_group=_int32("make_balance", bal, "tokens_per_group", 0),
                    unit=BALANCE_UNITS[bal.get("unit", "tokens")], weight=float(bal.get("weight", 1.0)))
 
 
