@@ -381,11 +381,14 @@ struct BalanceShape {
     int group, groups, pieces, piece, waves;   // count
     int cols, slabs, parts, steps;             // gradient
 };
+int balance_groups(const unif_moe_config* c, const unif_moe_balance* b) {
+    return b->tokens_per_group > 0 ? div_up(c->n_tokens, b->tokens_per_group) : 1;
+}
 BalanceShape balance_shape(const unif_moe_config* c, const unif_moe_balance* b, int cus) {
     BalanceShape s;
     const int N = std::max(c->n_tokens, 1);
     s.group = b->tokens_per_group > 0 ? b->tokens_per_group : N;
-    s.groups = b->tokens_per_group > 0 ? div_up(c->n_tokens, s.group) : 1;
+    s.groups = balance_groups(c, b);
     const int longest = std::min(s.group, N);
     s.piece = longest <= kBalOnePiece ? longest : std::max(kBalPiece, div_up(div_up(longest, kBalPieces), 64) * 64);
     s.pieces = div_up(longest, s.piece);
@@ -474,18 +477,18 @@ int32_t unif_moe_balance_loss(const unif_moe_config* cfg, const unif_moe_balance
         if (!aligned_to(q, 4)) return UNIF_EINVAL;
     const BalancePlan plan = plan_balance(cfg, bal);
     if (workspace == nullptr || workspace_bytes < plan.total) return UNIF_EWORKSPACE;
-    const BalanceShape sh = balance_shape(cfg, bal, std::min(cu_count(), kMaxCus));
     const size_t nd = (size_t)N * d, wb = 4 * (size_t)(K + 1) * d;
     static const unif_moe_routing no_record{};
     const unif_moe_routing& rec = N > 0 ? *record : no_record;
     const Span no(nullptr, 0);
-    const Span out[] = {Span(loss, 4), Span(counts, 8 * (size_t)sh.groups * (K + 1)), Span(dX, 4 * nd),
+    const Span out[] = {Span(loss, 4), Span(counts, 8 * (size_t)balance_groups(cfg, bal) * (K + 1)), Span(dX, 4 * nd),
                         Span(dW_router, wb), Span(workspace, plan.total)};
     const Span partner[] = {no, no, Span(dX_in, 4 * nd), Span(dW_router_in, wb), no};
     const Span in[] = {Span(valid, N), Span(X, nd * elem_size(cfg->dtype)), Span(W_router, wb),
                        Span(rec.n_shared, 4 * (size_t)N), Span(rec.n_res, 4 * (size_t)N),
                        Span(rec.expert_ids, 4 * (size_t)N * K), Span(rec.weights, 4 * (size_t)N * K)};
     if (!apart(out, partner, in)) return UNIF_EINVAL;
+    const BalanceShape sh = balance_shape(cfg, bal, std::min(cu_count(), kMaxCus));
     char* ws = align_base(workspace);
     BalanceParams p{};
     p.N = N;
