@@ -485,7 +485,8 @@ int32_t unif_moe_balance_loss(const unif_moe_config* cfg, const unif_moe_balance
                         Span(dW_router, wb), Span(workspace, plan.total)};
     const Span partner[] = {no, no, Span(dX_in, 4 * nd), Span(dW_router_in, wb), no};
     const Span in[] = {Span(valid, N), Span(X, nd * elem_size(cfg->dtype)), Span(W_router, wb),
-                       Span(rec.n_shared, 4 * (size_t)N), Span(rec.n_res, 4 * (size_t)N),
+                       Span(rec.alpha, 4 * (size_t)N), Span(rec.n_shared, 4 * (size_t)N),
+                       Span(rec.shared_mask, 8 * (size_t)N), Span(rec.n_res, 4 * (size_t)N),
                        Span(rec.expert_ids, 4 * (size_t)N * K), Span(rec.weights, 4 * (size_t)N * K)};
     if (!apart(out, partner, in)) return UNIF_EINVAL;
     const BalanceShape sh = balance_shape(cfg, bal, std::min(cu_count(), kMaxCus));
