@@ -76,7 +76,7 @@ size_t gate_bytes(const unif_moe_residual* r) { return (size_t)gate_rows(r) * r-
 bool gate_grouped(const unif_moe_residual* r) { return r->gate != nullptr && gate_rows(r) > 1; }
 
 // LDS that the kernels declare beside what their launch asks for.
-constexpr size_t kTeamLds = 2 * kWideWaves * 4 * sizeof(float), kCountLds = kBalWaves * (kWave * 12 + 8) + 4 * kWave,
+constexpr size_t kTeamLds = kWideWaves * (8 * sizeof(float) + sizeof(int)), kCountLds = kBalWaves * (kWave * 12 + 8) + 4 * kWave,
                  kSlopeLds = 8 * (kWave * kBalWaves + 2 * kWave + 2) + 4 * kWave;
 
 // Lanes per row (0: the workgroup) and the launch that covers the tokens.
@@ -197,12 +197,12 @@ ResidualParams residual_params(const unif_moe_residual* r, const RowShape& s) {
     return p;
 }
 
-// Workspace of the backward: four partial rows per workgroup
-// and a team's two pieces of shared gate groups, for the launch of any number
-// of compute units up to kMaxCus (the size is known without a device).
+// Workspace of the backward: four partial rows and a flag per workgroup, and a
+// team's two pieces of shared gate groups, for the launch of any number of compute
+// units up to kMaxCus (the size is known without a device).
 constexpr int kMaxCus = 512;
 struct ResidualPlan {
-    size_t part, gate_part, total;
+    size_t part, seen, gate_part, total;
 };
 ResidualPlan plan_residual(const unif_moe_residual* r) {
     const RowShape s = backward_shape(r, kMaxCus);
@@ -210,6 +210,7 @@ ResidualPlan plan_residual(const unif_moe_residual* r) {
     Carver cv;
     ResidualPlan p;
     p.part = cv.take(4 * row * s.blocks);
+    p.seen = cv.take(sizeof(int) * (size_t)s.blocks);
     p.gate_part = cv.take(gate_grouped(r) ? 2 * row * s.teams() : 0);
     p.total = cv.cur + 256;
     return p;
@@ -331,6 +332,7 @@ int32_t unif_moe_residual_backward(const unif_moe_residual* res, const void* y, 
     p.part = reinterpret_cast<float*>(ws + plan.part);
     p.gate_part = reinterpret_cast<float*>(ws + plan.gate_part);
     p.dgate = p.grouped ? gr.gate : nullptr;
+    p.seen = valid != nullptr && !p.grouped && res->gate != nullptr ? reinterpret_cast<int*>(ws + plan.seen) : nullptr;
     const bool one_gate = !p.grouped && gr.gate != nullptr;   // from the sums of out_gamma and out_beta
     p.want = (gr.out_gamma != nullptr || one_gate ? 1 << kSumOutGamma : 0) |
              (gr.out_beta != nullptr || one_gate ? 1 << kSumOutBeta : 0) |
@@ -348,7 +350,7 @@ int32_t unif_moe_residual_backward(const unif_moe_residual* res, const void* y, 
         const int by_wave = p.group / p.rows <= kFinishWaves;
         const ResidualFinish fin{p.N, p.d, sh.blocks, sh.teams(), p.group, p.rows, gate_rows(res), by_wave, p.grouped, p.part,
                                  p.gate_part, res->out_gamma, res->out_beta, res->gate,
-                                 {gr.out_gamma, gr.out_beta, gr.in_gamma, gr.in_beta}, gr.gate};
+                                 {gr.out_gamma, gr.out_beta, gr.in_gamma, gr.in_beta}, gr.gate, p.seen};
         int64_t shared = p.dgate != nullptr ? std::min<int64_t>(sh.teams() - 1, gate_rows(res)) : 0;
         if (by_wave) shared = (shared + kFinishWaves - 1) / kFinishWaves;
         residual_finish_kernel<<<dim3((unsigned)div_up(p.d, kWave), (unsigned)(4 + shared)), kFinishWaves * kWave, 0,

@@ -42,6 +42,7 @@ struct ResidualParams {
     float* dgate;              // [groups][d]: groups that one team holds (NULL: one gate row, or not wanted)
     int grouped;               // the gate has several rows
     int want;                  // bit i: partial sum i is wanted
+    int* seen;                 // [workgroups]: whether one had a real token (NULL: not needed, see residual_finish_kernel)
 };
 
 // kCols consecutive elements of a row, kCols = 4. Rows start at any element, so the
@@ -372,7 +373,9 @@ __global__ __launch_bounds__(LPR == 0 ? kWideWaves * kWave : 256) void residual_
 // (residual_finish_kernel adds those). A gate with several rows: a team that
 // comes to the end of a gate row's tokens adds its two sums, times the gate, to
 // its totals in LDS and writes that row's gradient, straight to the result
-// where it held all of its tokens, else as its first or last piece.
+// where it held all of its tokens, else as its first or last piece. Parameters may
+// be NaN or infinite where only padded tokens meet them (the gate row of an empty
+// sequence, say): they are multiplied only with what real tokens left.
 // 50,432 x 768 bf16 with fp32 dh: 120 us of 125, 4.5 TB/s of 14 bytes an element; the
 // registers (four sums, two parameter rows, four rows in flight) leave two waves
 // per SIMD, which is what keeps it from the copy's rate.
@@ -381,6 +384,7 @@ constexpr int kSumOutGamma = 0, kSumOutBeta = 1, kSumInGamma = 2, kSumInBeta = 3
 template <class S, class L, class H, int CH, int LPR>
 __global__ __launch_bounds__(LPR == 0 ? kWideWaves * kWave : 512) void residual_backward_kernel(ResidualParams p) {
     __shared__ float red[2 * kWideWaves * 4];
+    __shared__ int seen_by[kWideWaves];
     extern __shared__ float sums[];   // [teams of the workgroup][2][d]
     Team<LPR> team{red, 0};
     const Cols<CH> k(p.d, team.size(), team.sub());
@@ -407,6 +411,7 @@ __global__ __launch_bounds__(LPR == 0 ? kWideWaves * kWave : 512) void residual_
     float ig[CH][kCols], cg[CH][kCols];   // cg = gate gamma_out
     k.param(p.in_gamma, 1.f, ig);
     int64_t g = -1, gend = r0;
+    bool seen = false;   // a real token since the last flush
     auto flush = [&]() {
         const int64_t g0 = g * p.group, g1 = gend < p.N ? gend : p.N;
         float* const dst = (g0 >= r0 && g1 <= r1) ? p.dgate + g * p.d
@@ -416,8 +421,11 @@ __global__ __launch_bounds__(LPR == 0 ? kWideWaves * kWave : 512) void residual_
             k.param(p.out_gamma, 1.f, w);
             k.param(p.out_beta, 0.f, v);
             UNIF_COLS(c, e) w[c][e] = fmaf(w[c][e], acc[kSumOutGamma][c][e], v[c][e] * acc[kSumOutBeta][c][e]);
+            if (!seen) UNIF_COLS(c, e) w[c][e] = 0.f;
             k.store(dst, w);
         }
+        if (!seen) return;   // both sums are 0
+        seen = false;
         k.param(p.gate + g * p.d, 1.f, w);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -442,6 +450,8 @@ __global__ __launch_bounds__(LPR == 0 ? kWideWaves * kWave : 512) void residual_
         float y[CH][kCols], D[CH][kCols], f[CH][kCols];
         yr.get(k, y);
         fr.get(k, f);
+        const bool keep = real;
+        seen |= keep;
         real = is_real(r + 1);
         const int64_t ahead = real ? r + 1 : r;
         yr.load(k, ahead, real);
@@ -472,6 +482,7 @@ __global__ __launch_bounds__(LPR == 0 ? kWideWaves * kWave : 512) void residual_
         gr.get(k, dy);
         gr.load(k, ahead, real);
         UNIF_COLS(c, e) D[c][e] += dy[c][e];
+        if (!keep) UNIF_COLS(c, e) D[c][e] = 0.f;
         if (p.dx != nullptr) {
             UNIF_COLS(c, e) dy[c][e] = p.scale * D[c][e];
             k.store(static_cast<S*>(p.dx) + at, dy);
@@ -484,6 +495,7 @@ __global__ __launch_bounds__(LPR == 0 ? kWideWaves * kWave : 512) void residual_
         }
         if (p.df != nullptr) {
             if (p.out_norm != kNormNone) normalise_grad<CH, LPR>(team, p.out_norm, r_out, p.inv_d, f, D);
+            if (!keep) UNIF_COLS(c, e) D[c][e] = 0.f;
             k.store(static_cast<L*>(p.df) + at, D);
         }
     }
@@ -493,6 +505,10 @@ __global__ __launch_bounds__(LPR == 0 ? kWideWaves * kWave : 512) void residual_
     } else {
         k.store(mine, acc[kSumOutGamma]);
         k.store(mine + p.d, acc[kSumOutBeta]);
+    }
+    if (p.seen != nullptr) {
+        const uint64_t b = ballot(seen);
+        if (lane_id() == 0) seen_by[threadIdx.x >> 6] = b != 0;
     }
     // The teams' sums in team order, one partial row each per workgroup.
     const int nteam = (int)blockDim.x / team.size();
@@ -508,6 +524,11 @@ __global__ __launch_bounds__(LPR == 0 ? kWideWaves * kWave : 512) void residual_
         }
     };
     add_teams(kSumOutGamma);
+    if (p.seen != nullptr && threadIdx.x == 0) {
+        int any = 0;
+        for (int i = 0; i < (int)blockDim.x >> 6; ++i) any |= seen_by[i];
+        p.seen[blockIdx.x] = any;
+    }
     __syncthreads();
     k.store(mine, acc[kSumInGamma]);
     k.store(mine + p.d, acc[kSumInBeta]);
@@ -526,6 +547,7 @@ struct ResidualFinish {
     const float* gate;
     float* d_sum[4];         // gradients of the parameters by their sum (NULL: not wanted)
     float* d_gate;
+    const int* seen;         // [parts]: a workgroup had a real token (NULL: every one did)
 };
 
 // 64 columns per workgroup, the waves a stretch of the partial rows each, the
@@ -534,12 +556,15 @@ struct ResidualFinish {
 // rows whose tokens several teams share. Those are found from the ends of the
 // teams' tokens, or, where there are fewer, from the gate rows: a row belongs to
 // the first team's end that lies inside it. A gate row that few teams share is
-// one wave's, so that a workgroup takes as many as it has waves. Latency bound: 4 to
+// one wave's, so that a workgroup takes as many as it has waves. A single gate row
+// and N_out's parameters are multiplied here and so only where a real token met
+// them: `seen` tells, where tokens may be padded. Latency bound: 4 to
 // 7 us (253 partial rows of 768, 256 gate rows: 5.0; 16 waves where 4 took 14).
 constexpr int kFinishWaves = 16;
 
 __global__ __launch_bounds__(kFinishWaves* kWave) void residual_finish_kernel(ResidualFinish p) {
     __shared__ double stretch[2][kFinishWaves][kWave];
+    __shared__ int seen[kFinishWaves];
     const int lane = lane_id(), w = (int)threadIdx.x >> 6, n = (int)blockIdx.x * kWave + lane;
     // sum of rows k0 to k1 of src, `stride` floats apart
     auto column = [&](const float* src, int64_t k0, int64_t k1, size_t stride) {
@@ -578,8 +603,23 @@ __global__ __launch_bounds__(kFinishWaves* kWave) void residual_finish_kernel(Re
         const float* const src = p.part + (size_t)i * p.parts * p.d + n;
         stretch[0][w][lane] = n < p.d ? part_of(src, p.parts, p.d) : 0.0;
         stretch[1][w][lane] = gate && n < p.d ? part_of(src + (size_t)p.parts * p.d, p.parts, p.d) : 0.0;
+        if (p.seen != nullptr) {
+            int any = 0;
+            for (int k = (int)threadIdx.x; k < p.parts; k += (int)blockDim.x) any |= p.seen[k];
+            const uint64_t b = ballot(any != 0);
+            if (lane == 0) seen[w] = b != 0;
+        }
         __syncthreads();
         if (w != 0 || n >= p.d) return;
+        if (p.seen != nullptr) {
+            int any = 0;
+            for (int k = 0; k < kFinishWaves; ++k) any |= seen[k];
+            if (any == 0) {
+                if (out != nullptr) out[n] = 0.f;
+                if (gate) p.d_gate[n] = 0.f;
+                return;
+            }
+        }
         const double s = total(0);
         if (out != nullptr) out[n] = (float)(i <= kSumOutBeta && !p.grouped && p.gate != nullptr ? s * (double)p.gate[n] : s);
         if (gate)
