@@ -432,6 +432,8 @@ __global__ __launch_bounds__(kBalStrips * kWave, balance_waves(16 * KT) / 4) voi
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt) al[q][kt] = dl[kt];
         }
+    };
+    auto rows_flag = [&](int64_t t) {
         if (check) flag = p.valid[t + lr < p.N ? t + lr : p.N - 1];
     };
     auto rows_s = [&](int64_t t, f_raw (&so)[4], f32x4 (&ao)[KT]) {
@@ -451,15 +453,15 @@ __global__ __launch_bounds__(kBalStrips * kWave, balance_waves(16 * KT) / 4) voi
             ao[kt] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const char*>(p.dl + (size_t)t * KP) +
                                                      (k * KP + (uint32_t)lq * 4 * KT + 4 * kt) * 4u);
     };
+    rows_flag(first);
     if (want_w) rows_x(first);
     if (want_x) rows_s(first, s, ar);
     for (int64_t t = first; t < end; t += 16) {
         const int64_t next = t + 16 < end ? t + 16 : t;
+        uint32_t mask = 0xffffu;   // the step's real tokens
+        if (check) mask = (uint32_t)ballot(flag != 0) & 0xffffu;
+        if (t + 16 > end) mask &= (1u << (int)(end - t)) - 1;
         if (want_w) {
-            const bool tail = t + 16 > end;
-            uint32_t mask = 0xffffu;
-            if (check) mask = (uint32_t)ballot(flag != 0) & 0xffffu;
-            if (tail) mask &= (1u << (int)(end - t)) - 1;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 float b[NC];
@@ -478,6 +480,7 @@ __global__ __launch_bounds__(kBalStrips * kWave, balance_waves(16 * KT) / 4) voi
             }
             rows_x(next);
         }
+        rows_flag(next);
         if (want_x) {
             rows_s(next, sn, an);
             f32x4 acc[NC];
@@ -493,6 +496,7 @@ __global__ __launch_bounds__(kBalStrips * kWave, balance_waves(16 * KT) / 4) voi
                 f_raw v;   // dX_in is added last: one rounding at its magnitude
 #pragma unroll
                 for (int i = 0; i < NC; ++i) v[i] = s[r][i] + acc[i][r];
+                if (mask != 0xffffu && !(mask >> (4 * lq + r) & 1)) v = s[r];   // whatever the router's rows hold
                 if (t + 4 * lq + r < end) {
                     char* const out = reinterpret_cast<char*>(p.dX) + (size_t)(t + r) * p.d * 4 + ((uint32_t)lq * 4 * p.d + at) * 4u;
                     if (own == 0 && p.past) __builtin_nontemporal_store(v, reinterpret_cast<f_mem*>(out));
