@@ -206,7 +206,6 @@ class DeviceBlock:
     """
 
     def __init__(self, layer, params, stream_dtype=None):
-        import torch
         self.layer, self.params = layer, dict(params)
         c = layer.cfg
         size = dict(n_tokens=c["n_tokens"], d_model=c["d_model"], dtype=c["dtype"],
@@ -215,7 +214,6 @@ class DeviceBlock:
         behind = {k: v for k, v in params.items() if k not in before}
         self.before = ops.make_residual(dict(size, **before))
         self.behind = ops.make_residual(dict(size, **behind))
-        self.stream = torch.bfloat16 if size["stream_dtype"] == "bf16" else torch.float32
 
     @_on_stream
     def forward(self, x, *, stream=None):
