@@ -69,8 +69,8 @@ typedef struct unif_moe_residual {
  *   f      [N, d] dtype, or NULL: no branch (v = residual_scale * x; out_norm
  *          must be NONE and gate NULL). x or f must be given
  *   valid  [N] uint8, nonzero = real token; NULL means all valid. Padded
- *          tokens are skipped: their rows of y and h are zero, whatever x and
- *          f hold there
+ *          tokens are skipped: their rows of y and h are zero, whatever x, f and
+ *          parameters hold there (a gate row that only padded tokens have)
  *   y      [N, d] stream_dtype, or NULL: not written. May be x itself
  *   h      [N, d] dtype, or NULL: not written; needs in_norm other than NONE
  * Other overlaps of outputs with inputs or each other are rejected. Tensors
@@ -105,7 +105,8 @@ int32_t unif_moe_residual_backward_workspace_size(const unif_moe_residual* res, 
  *   f      [N, d] dtype: the forward's branch; needed for df and the gradients
  *          of gate and N_out unless out_norm is NONE and only df is wanted
  *   valid  as in the forward: padded tokens get dx = df = 0 and add nothing to
- *          any gradient, whatever the inputs hold there
+ *          any gradient, whatever the inputs and parameters hold there; the
+ *          gradient of a gate row that only padded tokens have is 0
  *   dy     [N, d] stream_dtype, or NULL (0)
  *   dh     [N, d] dh_dtype, or NULL (0); needs in_norm other than NONE. dy or
  *          dh must be given
@@ -161,7 +162,8 @@ int32_t unif_moe_balance_loss_workspace_size(const unif_moe_config* cfg, const u
  *   counts     [G, K+1] int64, written, or NULL: column j the load c_sj, column
  *              0 the shared expert's (valid tokens, or their blocks sum b)
  *   dX_in      [N, d] fp32 or NULL (0); may be dX itself (added in place)
- *   dX         [N, d] fp32, or NULL: not wanted. Padded tokens get dX_in's rows
+ *   dX         [N, d] fp32, or NULL: not wanted. Padded tokens get dX_in's rows,
+ *              whatever W_router holds
  *   dW_router_in, dW_router   [K+1, d] fp32, likewise
  * A training step calls it after unif_moe_layer_backward with the layer's
  * gradients in place. cfg is validated as for the layer; N, d, K, B and dtype

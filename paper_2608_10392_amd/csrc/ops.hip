@@ -114,9 +114,13 @@ RowShape cover(RowShape s, int N, int cus, int waves) {
 }
 
 // Outputs past this size do not stay in the L2s (8 x 4 MB) for the next kernel
-// and are stored around them: join of 131,072 x 1,024 with an fp32 stream 301 ->
-// 285 us, balance gradients of the same size, K = 32, 315 -> 306. (The join's
-// gradients gain nothing: 50,432 x 768 125.8 and 127.3.)
+// and are stored around them: join of 131,072 x 1,024 with an fp32 stream 304 ->
+// 286 us, of 50,432 x 768 57 -> 49; balance gradients of 131,072 x 1,024, K = 32,
+// 315 -> 306 in an earlier form. (The join's gradients gain nothing: 50,432 x 768
+// 125.8 and 127.3.) Together with the kernel that reads the output next it gains
+// nothing: the join and a pass over h 390 and 388 us at 131,072 x 1,024, 83 and 85 at
+// 50,432 x 768; the balance gradients and the gradient of N_in 609 and 607, 161 and
+// 160.
 constexpr size_t kCacheBytes = (size_t)32 << 20;
 
 // Calls f(chunks, lanes per row) for a launch's shape.
@@ -146,10 +150,12 @@ RowShape forward_shape(const unif_moe_residual* r, int cus) {
     if (r->d_model > kNarrowD) return cover(wide_shape(r->d_model), r->n_tokens, cus, 16);
     return cover(narrow_shape(r->d_model, 256), r->n_tokens, cus, 64);
 }
-// Backward: as many waves as run at once (two per SIMD, by their registers), so
-// that the partial rows are few: 50,432 x 768 134 us with 8 waves per compute
-// unit, 168 with 4, 158 with 24. Wide rows in 2 chunks a lane: 16,384 x 4,096
-// 170 us, in 3 212, in 4 184; 4,099 x 5,120 72, 78 and 79.
+// Backward: as many waves as run at once (two per SIMD by the registers of 3 and 4
+// chunks a lane), so that the partial rows are few: 50,432 x 768 134 us with 8 waves
+// per compute unit, 168 with 4, 158 with 24. The kernels of 2 chunks a lane take 137
+// to 170 registers, and most would run three per SIMD; they are launched alike, which
+// was not measured for them. Wide rows in 2 chunks a lane: 16,384 x 4,096 170 us, in 3
+// 212, in 4 184; 4,099 x 5,120 72, 78 and 79.
 RowShape backward_shape(const unif_moe_residual* r, int cus) {
     return cover(r->d_model > kNarrowD ? wide_shape(r->d_model) : narrow_shape(r->d_model, 512), r->n_tokens, cus, 8);
 }

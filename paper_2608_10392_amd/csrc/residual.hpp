@@ -308,9 +308,9 @@ __device__ __forceinline__ void normalise_grad(Team<LPR>& team, int norm, float 
 }
 
 // PAST: the outputs are larger than the caches and stored around them.
-// 50,432 x 768 bf16, both norms and a gate per 197 tokens: 64 us, 4.8 TB/s of the
+// 50,432 x 768 bf16, both norms and a gate per 197 tokens: 62 us, 5.0 TB/s of the
 // 8 bytes an element (a copy runs at 5.15); 131,072 x 1,024 with an fp32 stream:
-// 286 us, 5.6 TB/s of 12 bytes; one token 3.3 us, a launch.
+// 287 us, 5.6 TB/s of 12 bytes; one token 3.3 us, a launch.
 template <class S, class L, bool PAST, int CH, int LPR>
 __global__ __launch_bounds__(LPR == 0 ? kWideWaves * kWave : 256) void residual_forward_kernel(ResidualParams p) {
     __shared__ float red[2 * kWideWaves * 4];
@@ -376,9 +376,12 @@ __global__ __launch_bounds__(LPR == 0 ? kWideWaves * kWave : 256) void residual_
 // where it held all of its tokens, else as its first or last piece. Parameters may
 // be NaN or infinite where only padded tokens meet them (the gate row of an empty
 // sequence, say): they are multiplied only with what real tokens left.
-// 50,432 x 768 bf16 with fp32 dh: 120 us of 125, 4.5 TB/s of 14 bytes an element; the
+// 50,432 x 768 bf16 with fp32 dh: 119 us of 125, 4.5 TB/s of 14 bytes an element; the
 // registers (four sums, two parameter rows, four rows in flight) leave two waves
-// per SIMD, which is what keeps it from the copy's rate.
+// per SIMD, which is what keeps it from the copy's rate. Rows of 769 to 1,024 columns (4
+// chunks) spill 8 to 24 registers but in bf16 throughout, and wide rows, whose teams may
+// have 16 waves and so 128 registers a lane, 17 to 37: 8 of the 107 MB that 4,099 x
+// 5,120 writes.
 constexpr int kSumOutGamma = 0, kSumOutBeta = 1, kSumInGamma = 2, kSumInBeta = 3;
 
 template <class S, class L, class H, int CH, int LPR>
