@@ -357,10 +357,10 @@ __global__ __launch_bounds__(1024) void balance_mean_kernel(BalanceParams p) { b
 // branch (a step past the range re-reads the last, rows past the last token the
 // last row), and the stores come last: the waits at the next step then name loads
 // a whole product old. (The flags of padded tokens loaded ahead of the first product
-// instead: 50,000 x 1,024, K = 64, half of them padded, 213 -> 229 us.) Padded tokens
+// instead: 50,000 x 1,024, K = 64, half of them padded, 209 -> 229 us.) Padded tokens
 // have dl = 0, their rows of X are not used, and their rows of dX take no product.
 // HBM bound: 50,432 x 768 bf16, K = 16 84 us, 4.6 TB/s of 10 bytes an element;
-// 131,072 x 1,024, K = 32 288 us, 4.7 TB/s, the matrix cores busy 40% of it at 153
+// 131,072 x 1,024, K = 32 279 to 288 us, 4.7 TB/s, the matrix cores busy 40% of it at 153
 // TFLOP/s. Past 48 experts the products take as long as the memory (50,000 x 1,024,
 // K = 64 175 us against 100), and where dX is added or one gradient is wanted alone the
 // kernel spills 12 to 22 registers. The router in LDS and a third wave per SIMD instead:
@@ -456,8 +456,8 @@ __global__ __launch_bounds__(kBalStrips * kWave, balance_waves(16 * KT) / 4) voi
             ao[kt] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const char*>(p.dl + (size_t)t * KP) +
                                                      (k * KP + (uint32_t)lq * 4 * KT + 4 * kt) * 4u);
     };
-    rows_flag(first);
     if (want_w) rows_x(first);
+    rows_flag(first);
     if (want_x) rows_s(first, s, ar);
     for (int64_t t = first; t < end; t += 16) {
         const int64_t next = t + 16 < end ? t + 16 : t;
