@@ -208,15 +208,14 @@ ResidualParams residual_params(const unif_moe_residual* r, const RowShape& s) {
 // units up to kMaxCus (the size is known without a device).
 constexpr int kMaxCus = 512;
 struct ResidualPlan {
-    size_t part, seen, gate_part, total;
+    size_t part, gate_part, total;
 };
 ResidualPlan plan_residual(const unif_moe_residual* r) {
     const RowShape s = backward_shape(r, kMaxCus);
     const size_t row = (size_t)r->d_model * sizeof(float);
     Carver cv;
     ResidualPlan p;
-    p.part = cv.take(4 * row * s.blocks);
-    p.seen = cv.take(sizeof(int) * (size_t)s.blocks);
+    p.part = cv.take((4 * row + sizeof(int)) * s.blocks);
     p.gate_part = cv.take(gate_grouped(r) ? 2 * row * s.teams() : 0);
     p.total = cv.cur + 256;
     return p;
@@ -338,11 +337,13 @@ int32_t unif_moe_residual_backward(const unif_moe_residual* res, const void* y, 
     p.part = reinterpret_cast<float*>(ws + plan.part);
     p.gate_part = reinterpret_cast<float*>(ws + plan.gate_part);
     p.dgate = p.grouped ? gr.gate : nullptr;
-    p.seen = valid != nullptr && !p.grouped && res->gate != nullptr ? reinterpret_cast<int*>(ws + plan.seen) : nullptr;
     const bool one_gate = !p.grouped && gr.gate != nullptr;   // from the sums of out_gamma and out_beta
     p.want = (gr.out_gamma != nullptr || one_gate ? 1 << kSumOutGamma : 0) |
              (gr.out_beta != nullptr || one_gate ? 1 << kSumOutBeta : 0) |
              (gr.in_gamma != nullptr ? 1 << kSumInGamma : 0) | (gr.in_beta != nullptr ? 1 << kSumInBeta : 0);
+    // a single gate row's products wait for the finishing launch, which has to know of real tokens
+    const bool flags = valid != nullptr && !p.grouped && res->gate != nullptr && (p.want & (1 << kSumOutGamma | 1 << kSumOutBeta)) != 0;
+    if (flags) p.want |= 1 << kSeen;
     int32_t status;
     if (res->dtype == UNIF_F32) status = launch_backward<float, float, float>(sh, p, st);
     else if (res->stream_dtype == UNIF_F32 && dh_dtype == UNIF_F32)
@@ -354,9 +355,10 @@ int32_t unif_moe_residual_backward(const unif_moe_residual* res, const void* y, 
     UNIF_LAUNCH_CHECK();
     if (p.want != 0 || p.dgate != nullptr) {
         const int by_wave = p.group / p.rows <= kFinishWaves;
+        const int* const seen = flags ? reinterpret_cast<const int*>(p.part + (size_t)4 * sh.blocks * p.d) : nullptr;
         const ResidualFinish fin{p.N, p.d, sh.blocks, sh.teams(), p.group, p.rows, gate_rows(res), by_wave, p.grouped, p.part,
                                  p.gate_part, res->out_gamma, res->out_beta, res->gate,
-                                 {gr.out_gamma, gr.out_beta, gr.in_gamma, gr.in_beta}, gr.gate, p.seen};
+                                 {gr.out_gamma, gr.out_beta, gr.in_gamma, gr.in_beta}, gr.gate, seen};
         int64_t shared = p.dgate != nullptr ? std::min<int64_t>(sh.teams() - 1, gate_rows(res)) : 0;
         if (by_wave) shared = (shared + kFinishWaves - 1) / kFinishWaves;
         residual_finish_kernel<<<dim3((unsigned)div_up(p.d, kWave), (unsigned)(4 + shared)), kFinishWaves * kWave, 0,

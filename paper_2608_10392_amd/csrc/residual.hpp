@@ -37,12 +37,11 @@ struct ResidualParams {
     const void* dh;
     void* dx;
     void* df;
-    float* part;               // [4][workgroups][d] partial sums (kSum*)
+    float* part;               // [4][workgroups][d] partial sums (kSum*), then a flag per workgroup (kSeen)
     float* gate_part;          // [teams][2][d]: a team's first and last piece of gate groups it shares
     float* dgate;              // [groups][d]: groups that one team holds (NULL: one gate row, or not wanted)
     int grouped;               // the gate has several rows
-    int want;                  // bit i: partial sum i is wanted
-    int* seen;                 // [workgroups]: whether one had a real token (NULL: not needed, see residual_finish_kernel)
+    int want;                  // bit i: partial sum i is wanted; bit kSeen: the flags, whether one had a real token
 };
 
 // kCols consecutive elements of a row, kCols = 4. Rows start at any element, so the
@@ -380,9 +379,9 @@ __global__ __launch_bounds__(LPR == 0 ? kWideWaves * kWave : 256) void residual_
 // registers (four sums, two parameter rows, four rows in flight) leave two waves
 // per SIMD, which is what keeps it from the copy's rate. Rows of 769 to 1,024 columns (4
 // chunks) spill 8 to 24 registers but in bf16 throughout, and wide rows, whose teams may
-// have 16 waves and so 128 registers a lane, 17 to 37: 8 of the 107 MB that 4,099 x
+// have 16 waves and so 128 registers a lane, 17 to 37: 10 of the 109 MB that 4,099 x
 // 5,120 writes.
-constexpr int kSumOutGamma = 0, kSumOutBeta = 1, kSumInGamma = 2, kSumInBeta = 3;
+constexpr int kSumOutGamma = 0, kSumOutBeta = 1, kSumInGamma = 2, kSumInBeta = 3, kSeen = 4;
 
 template <class S, class L, class H, int CH, int LPR>
 __global__ __launch_bounds__(LPR == 0 ? kWideWaves * kWave : 512) void residual_backward_kernel(ResidualParams p) {
@@ -509,7 +508,7 @@ __global__ __launch_bounds__(LPR == 0 ? kWideWaves * kWave : 512) void residual_
         k.store(mine, acc[kSumOutGamma]);
         k.store(mine + p.d, acc[kSumOutBeta]);
     }
-    if (p.seen != nullptr) {
+    if (p.want >> kSeen & 1) {
         const uint64_t b = ballot(seen);
         if (lane_id() == 0) seen_by[threadIdx.x >> 6] = b != 0;
     }
@@ -527,10 +526,10 @@ __global__ __launch_bounds__(LPR == 0 ? kWideWaves * kWave : 512) void residual_
         }
     };
     add_teams(kSumOutGamma);
-    if (p.seen != nullptr && threadIdx.x == 0) {
+    if ((p.want >> kSeen & 1) && threadIdx.x == 0) {
         int any = 0;
         for (int i = 0; i < (int)blockDim.x >> 6; ++i) any |= seen_by[i];
-        p.seen[blockIdx.x] = any;
+        reinterpret_cast<int*>(p.part + (size_t)4 * gridDim.x * p.d)[blockIdx.x] = any;
     }
     __syncthreads();
     k.store(mine, acc[kSumInGamma]);
@@ -550,7 +549,7 @@ struct ResidualFinish {
     const float* gate;
     float* d_sum[4];         // gradients of the parameters by their sum (NULL: not wanted)
     float* d_gate;
-    const int* seen;         // [parts]: a workgroup had a real token (NULL: every one did)
+    const int* seen;         // [parts]: whether a workgroup had a real token (NULL: every one did)
 };
 
 // 64 columns per workgroup, the waves a stretch of the partial rows each, the
