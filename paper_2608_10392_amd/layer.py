@@ -36,10 +36,11 @@ def to_device(a, dtype_name, device, name="array", shape=None):
 
 
 def _on_stream(method):
-    """Runs ``method`` with its ``stream`` argument (a torch stream, a raw handle
-    or None: the layer's device's current one) current, and so its device: what
-    it allocates belongs to that stream, so memory it frees on return is not
-    handed out before the stream's work on it is done."""
+    """Runs ``method`` with its ``stream`` argument (a torch stream, another
+    object's ``cuda_stream``, a raw handle, or None: the layer's device's current
+    one) current, and so its device: what it allocates belongs to that stream, so
+    memory it frees on return is not handed out before the stream's work on it is
+    done."""
     args_of = inspect.signature(method).parameters
     at = list(args_of).index("stream") - 1   # among the arguments behind self
     by_position = args_of["stream"].kind is inspect.Parameter.POSITIONAL_OR_KEYWORD
@@ -50,6 +51,8 @@ def _on_stream(method):
         given = by_position and len(args) > at
         stream = args[at] if given else kwargs.get("stream")
         device = getattr(self, "layer", self).Y.get_device()
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = getattr(stream, "cuda_stream", stream)
         if isinstance(stream, int):
             # 0 is the null stream's handle, which ExternalStream takes for none at all
             stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)

@@ -26,6 +26,7 @@ class Streams:
     def __init__(self, monkeypatch):
         self.now, self.seen = Stream(0), []
         cuda = torch.cuda
+        monkeypatch.setattr(cuda, "Stream", Stream)
         monkeypatch.setattr(cuda, "default_stream", lambda device=None: Stream(0))
         monkeypatch.setattr(cuda, "current_stream", lambda device=None: self.now)
         # as torch's: a handle of 0 counts as not given, a stream of torch's own comes back
@@ -46,6 +47,7 @@ class Streams:
 
     @contextlib.contextmanager
     def use(self, stream):
+        assert isinstance(stream, Stream)   # torch's takes no other
         was, self.now = self.now, stream
         yield
         self.now = was
@@ -70,12 +72,17 @@ NEW = dict(block_forward=lambda dev, block, **s: block.forward(X, **s),
 @pytest.mark.parametrize("name", list(NEW))
 def test_handles(name, monkeypatch):
     """A raw handle, 0 (the null stream) among them, is the stream that is used
-    and that the call's memory belongs to."""
+    and that the call's memory belongs to; so is another object's."""
     streams, (dev, block) = Streams(monkeypatch), make()
-    for handle in (0, 77):
+
+    class Foreign:
+        """Another library's stream."""
+        cuda_stream = 78
+
+    for given, handle in ((0, 0), (77, 77), (Foreign(), 78)):
         for now in (Stream(0), Stream(5)):
             streams.now, streams.seen = now, []
-            NEW[name](dev, block, stream=handle)
+            NEW[name](dev, block, stream=given)
             assert streams.seen and {s[1:] for s in streams.seen} == {(handle, handle)}, streams.seen
             assert streams.now is now
 
